@@ -19,6 +19,13 @@ The call names mirror the C entry points:
   aspis_sgd(g, w, v, eta, mu)               the model update with the aggregate (Eq. 1, momentum)
   aspis_detect_wide(adj, K, det)            Algorithm 3 for K <= 128 (graph given directly)
   aspis_round_tolerant(copies, d, a, tau, ...)   the round for copies that are not bit-identical
+
+and those of ``include/aspis_optim.h``, the end of a training step over a
+model's many tensors:
+
+  aspis_grad_norm(grads, norm, work)             their global norm
+  aspis_clip_grads(grads, max_norm, norm, work)  the norm and clipping by it
+  aspis_adamw(params, step, lr, ...)             AdamW with the clipping inside
 """
 from __future__ import annotations
 
@@ -105,6 +112,30 @@ def wide_detection_buffer(device, node_budget: int = 0, flags: int = 0):
     return host.to(device)
 
 
+NORM_WORKSPACE_BYTES = 32768
+F32, BF16, F16 = 0, 1, 2
+
+
+class _Tensor(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("out", ctypes.c_void_p), ("numel", ctypes.c_int64),
+                ("type", ctypes.c_int32), ("out_type", ctypes.c_int32)]
+
+
+class _Param(ctypes.Structure):
+    _fields_ = [("param", ctypes.c_void_p), ("master", ctypes.c_void_p), ("grad", ctypes.c_void_p),
+                ("exp_avg", ctypes.c_void_p), ("exp_avg_sq", ctypes.c_void_p),
+                ("numel", ctypes.c_int64), ("param_type", ctypes.c_int32),
+                ("grad_type", ctypes.c_int32), ("weight_decay", ctypes.c_float),
+                ("reserved", ctypes.c_int32)]
+
+
+class _AdamwArgs(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double), ("step", ctypes.c_int64), ("max_norm", ctypes.c_float),
+                ("scale", ctypes.c_float), ("skip_nonfinite", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is missing: build it first (python "
@@ -133,6 +164,16 @@ def _load():
         "aspis_round_tolerant": ([P, i64, i64, A, ctypes.c_float, P, P, P, P, P, P, i64, i32, P, P],
                                  i32),
     }
+    f32 = ctypes.c_float
+    sig.update({
+        "aspis_tensors_create": ([ctypes.POINTER(_Tensor), i64, ctypes.POINTER(P)], i32),
+        "aspis_tensors_destroy": ([P], None),
+        "aspis_params_create": ([ctypes.POINTER(_Param), i64, ctypes.POINTER(P)], i32),
+        "aspis_params_destroy": ([P], None),
+        "aspis_grad_norm": ([P, f32, P, P, P, P], i32),
+        "aspis_clip_grads": ([P, f32, f32, P, P, P], i32),
+        "aspis_adamw": ([P, ctypes.POINTER(_AdamwArgs), P, P, P], i32),
+    })
     for name, (args, res) in sig.items():
         fn = getattr(lib, name)
         fn.argtypes = args
@@ -372,3 +413,192 @@ class TolerantBuffers(RoundBuffers):
         super().__init__(a, d, device)
         self.slot_mask = torch.zeros(a.f, dtype=torch.uint8, device=device)
         self.means = torch.zeros((a.f, (d + 3) // 4 * 4), dtype=torch.float32, device=device)
+
+
+# ------------------------------------------------ many tensors (aspis_optim.h)
+
+
+def _types():
+    import torch
+    return {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+
+
+def _gapless(t):
+    """True when the tensor's elements fill its range of memory, in any order of dimensions."""
+    if t.is_contiguous():
+        return True
+    at = 1
+    for stride, size in sorted((st, n) for st, n in zip(t.stride(), t.shape) if n > 1):
+        if stride != at:
+            return False
+        at *= size
+    return True
+
+
+def _tensor(t, types, device, name):
+    """The tensor's type code, after the checks that every tensor of a list has to pass."""
+    import torch
+    if t.layout != torch.strided or not t.is_cuda:
+        raise ValueError(f"{name} must be dense CUDA tensors")
+    if t.device != device:
+        raise ValueError(f"{name} must be on one device: got {t.device} and {device}")
+    code = types.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
+    if not _gapless(t):
+        raise ValueError(f"{name} must fill their memory without gaps")
+    return code
+
+
+def _alike(t, other, name):
+    """Elementwise partners: the same shape, and the same order in memory."""
+    if t.shape != other.shape:
+        raise ValueError(f"{name}: shapes {tuple(t.shape)} and {tuple(other.shape)} differ")
+    if t.stride() != other.stride() and not (t.is_contiguous() and other.is_contiguous()):
+        raise ValueError(f"{name}: orders in memory (strides) differ")
+
+
+class _List:
+    """Owns a list handle, and keeps its tensors' memory."""
+    _create = _destroy = None
+
+    def __init__(self, items, n, device, kept):
+        self._h = ctypes.c_void_p()
+        self.n, self.device, self._kept = n, device, kept
+        _ok(getattr(lib, self._create)(items, n, ctypes.byref(self._h)), self._create)
+
+    def __len__(self):
+        return self.n
+
+    def close(self):
+        h, self._h = getattr(self, "_h", None), None
+        if h:
+            getattr(lib, self._destroy)(h)
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class TensorList(_List):
+    """Gradients for :func:`aspis_grad_norm` and :func:`aspis_clip_grads`.
+
+    ``out``: tensors of the same shapes for the clipped values (any of the three
+    types), or None to clip in place.  The list holds the tensors' memory as it is
+    now: make another when a gradient moves to other memory."""
+    _create, _destroy = "aspis_tensors_create", "aspis_tensors_destroy"
+
+    def __init__(self, tensors, out=None):
+        tensors = list(tensors)
+        outs = [None] * len(tensors) if out is None else list(out)
+        if len(outs) != len(tensors):
+            raise ValueError(f"{len(tensors)} tensors and {len(outs)} outputs")
+        types, device = _types(), tensors[0].device if tensors else None
+        items = (_Tensor * len(tensors))()
+        for item, t, o in zip(items, tensors, outs):
+            item.type = _tensor(t, types, device, "tensors")
+            item.data, item.numel = t.data_ptr(), t.numel()
+            if o is not None:
+                item.out_type = _tensor(o, types, device, "out")
+                _alike(t, o, "out")
+                item.out = o.data_ptr()
+        super().__init__(items, len(tensors), device,
+                         [t.detach() for t in tensors + [o for o in outs if o is not None]])
+
+
+class ParamList(_List):
+    """Parameters with their gradients and moments for :func:`aspis_adamw`.
+
+    ``exp_avg``, ``exp_avg_sq`` and ``masters`` are float32; ``masters`` (all of the
+    16-bit parameters', or None) hold the weights that the step is made on.
+    ``weight_decay``: one value, or one per tensor."""
+    _create, _destroy = "aspis_params_create", "aspis_params_destroy"
+
+    def __init__(self, params, grads, exp_avg, exp_avg_sq, masters=None, weight_decay=0.0):
+        params, grads, exp_avg, exp_avg_sq = (list(x) for x in (params, grads, exp_avg, exp_avg_sq))
+        n = len(params)
+        masters = [None] * n if masters is None else list(masters)
+        decay = [float(weight_decay)] * n if isinstance(weight_decay, (int, float)) else list(weight_decay)
+        for name, x in (("grads", grads), ("exp_avg", exp_avg), ("exp_avg_sq", exp_avg_sq),
+                        ("masters", masters), ("weight_decay", decay)):
+            if len(x) != n:
+                raise ValueError(f"{n} params and {len(x)} {name}")
+        types, device = _types(), params[0].device if n else None
+        items = (_Param * n)()
+        for item, p, g, m, v, w, k in zip(items, params, grads, exp_avg, exp_avg_sq, masters, decay):
+            item.param_type = _tensor(p, types, device, "params")
+            item.grad_type = _tensor(g, types, device, "grads")
+            for name, x in (("grads", g), ("exp_avg", m), ("exp_avg_sq", v), ("masters", w)):
+                if x is None:
+                    continue
+                if name != "grads" and _tensor(x, types, device, name) != F32:
+                    raise ValueError(f"{name} must be float32")
+                _alike(p, x, name)
+            item.param, item.grad, item.numel = p.data_ptr(), g.data_ptr(), p.numel()
+            item.exp_avg, item.exp_avg_sq = m.data_ptr(), v.data_ptr()
+            item.master = None if w is None else w.data_ptr()
+            item.weight_decay = k
+        super().__init__(items, n, device, [t.detach() for x in (params, grads, exp_avg, exp_avg_sq, masters)
+                                            for t in x if t is not None])
+
+
+class NormBuffers:
+    """Device buffers of a norm: ``norm`` (float32 [1]) and ``work``."""
+
+    def __init__(self, device="cuda"):
+        import torch
+        self.norm = torch.zeros(1, dtype=torch.float32, device=device)
+        self.work = torch.zeros(NORM_WORKSPACE_BYTES, dtype=torch.uint8, device=device)
+
+
+def _norm_args(norm, work):
+    import torch
+    if work is not None and work.numel() < NORM_WORKSPACE_BYTES:
+        raise ValueError(f"work must have {NORM_WORKSPACE_BYTES} bytes")
+    if norm is not None and norm.numel() < 1:
+        raise ValueError("norm must have an element")
+    return (None if norm is None else _dev(norm, torch.float32, "norm"),
+            None if work is None else _dev(work, torch.uint8, "work"))
+
+
+def _list_stream(x, stream):
+    if stream is None and x.device is not None:
+        import torch
+        return ctypes.c_void_p(torch.cuda.current_stream(x.device).cuda_stream)
+    return _stream(stream)
+
+
+def aspis_grad_norm(grads: TensorList, norm, work, tensor_norms=None, scale: float = 1.0, stream=None):
+    """norm <- scale * the global L2 norm of ``grads``; ``tensor_norms`` (float32 [n]):
+    every tensor's own."""
+    import torch
+    if tensor_norms is not None and tensor_norms.numel() < grads.n:
+        raise ValueError(f"tensor_norms must have {grads.n} elements")
+    np_, wp = _norm_args(norm, work)
+    _ok(lib.aspis_grad_norm(grads._h, scale, np_,
+                            None if tensor_norms is None else _dev(tensor_norms, torch.float32, "tensor_norms"),
+                            wp, _list_stream(grads, stream)), "aspis_grad_norm")
+
+
+def aspis_clip_grads(grads: TensorList, max_norm: float, norm, work=None, scale: float = 1.0, stream=None):
+    """Clips ``grads`` to ``max_norm`` (into the list's outputs, or in place) and writes
+    their norm; without ``work`` the norm is given in ``norm``."""
+    np_, wp = _norm_args(norm, work)
+    _ok(lib.aspis_clip_grads(grads._h, max_norm, scale, np_, wp, _list_stream(grads, stream)),
+        "aspis_clip_grads")
+
+
+def aspis_adamw(params: ParamList, step: int, lr: float, betas=(0.9, 0.999), eps: float = 1e-8,
+                max_norm=None, norm=None, work=None, scale: float = 1.0, skip_nonfinite: bool = False,
+                stream=None):
+    """One AdamW step (``step`` counts from 1).  ``max_norm``: clip by the global norm,
+    which is written to ``norm``, or given there where ``work`` is None; None: no
+    clipping.  ``skip_nonfinite``: change nothing where the norm is not finite."""
+    args = _AdamwArgs(lr, betas[0], betas[1], eps, step, -1.0 if max_norm is None else max_norm, scale,
+                      skip_nonfinite, 0)
+    if max_norm is not None and max_norm < 0:
+        raise ValueError("max_norm must not be negative")
+    np_, wp = _norm_args(norm, work)
+    _ok(lib.aspis_adamw(params._h, ctypes.byref(args), np_, wp, _list_stream(params, stream)), "aspis_adamw")

@@ -20,7 +20,7 @@ LIB = os.path.join(PKG, "libaspis.so")
 SOURCES = ["assign.cpp", "api.cu", "check.cu", "detect.cu", "aggregate.cu", "round.cu", "sweep_r1.cu", "sweep_r2.cu",
            "sweep_r3.cu", "sweep_r4.cu", "sweep_r5.cu", "few.cu",
            "round_static.cu", "update.cu", "detect_wide.cu",
-           "tolerant.cu"]
+           "tolerant.cu", "optim_list.cu", "norm.cu", "clip.cu", "adamw.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 
@@ -54,7 +54,7 @@ def _stale() -> bool:
         return True
     t = os.path.getmtime(LIB)
     deps = [os.path.join(CSRC, s) for s in os.listdir(CSRC)]
-    deps += [os.path.join(ROOT, "include", "aspis.h"), __file__]
+    deps += [os.path.join(ROOT, "include", h) for h in ("aspis.h", "aspis_optim.h")] + [__file__]
     return any(os.path.getmtime(x) > t for x in deps)
 
 
