@@ -1,5 +1,6 @@
 // aspis_adamw: the norm (norm.cu), then one AdamW step on every tensor with the
-// gradient read through the clipping coefficient.
+// gradient read through the clipping coefficient.  The step streams every array once, eight
+// elements per thread and access, and is bound by HBM.
 #include <math.h>
 
 #include "optim.cuh"
@@ -19,49 +20,108 @@ struct Step {
     int skip;
 };
 
-template <int N>
-__global__ void __launch_bounds__(kOptThreads)
-adamw_kernel(const __grid_constant__ Table<ParamEntry, N> t, const __grid_constant__ Step s, int param_type,
-             int grad_type)
+__device__ __forceinline__ void step_one(const Step &s, float c, float decay, float g, float &x, float &m, float &v)
 {
-    chain();
+    const float h = g * c;
+    m = fmaf(s.beta1, m, s.one_beta1 * h);
+    v = fmaf(s.beta2, v, s.one_beta2 * h * h);
+    x -= fmaf(decay, x, s.rate * (m / fmaf(sqrtf(v), s.root, s.eps)));
+}
+
+// Element i alone.
+template <int BP, int BG, bool MASTER>
+__device__ __forceinline__ void step_element(const ParamEntry &e, const Step &s, float c, float decay, int64_t i, bool bp,
+                                             bool bg)
+{
+    float x = MASTER ? e.master[i] : load_one<BP>(e.param, i, bp), m = e.m[i], v = e.v[i];
+    step_one(s, c, decay, load_one<BG>(e.grad, i, bg), x, m, v);
+    e.m[i] = m;
+    e.v[i] = v;
+    if (MASTER) e.master[i] = x;
+    store_one<BP>(e.param, i, x, bp);
+}
+
+// Units [ua, ub) of a tensor: groups of eight elements, one per thread, counted from the group
+// boundary at or before the first moment's first element.  The gradient may lie behind that boundary by
+// any number of elements (a view of a flat aggregate); arrays that are written and do not share
+// it are taken element by element.
+template <int BP, int BG, bool MASTER>
+__device__ __forceinline__ void step_units(const ParamEntry &e, const Step &s, float c, uint32_t ua, uint32_t ub, bool bp,
+                                           bool bg)
+{
+    const float decay = s.lr * e.decay;
+    const int h = behind<4>(e.m);
+    const int64_t first = (int64_t)ua * kParamUnit, last = (int64_t)ub * kParamUnit;
+    if (behind<4>(e.v) != h || behind<BP>(e.param) != h || (MASTER && behind<4>(e.master) != h)) {
+        for (int64_t i = first + threadIdx.x; i < min(last, e.numel); i += kOptThreads)
+            step_element<BP, BG, MASTER>(e, s, c, decay, i, bp, bg);
+        return;
+    }
+    const char *grad = static_cast<const char *>(e.grad);
+    char *param = static_cast<char *>(e.param);
+    const int shift = behind<BG>(grad - h * BG);
+    const int64_t end = min(last / 8, (e.numel + h + 7) / 8);
+    for (int64_t q = first / 8 + threadIdx.x; q < end; q += kOptThreads) {
+        const int64_t i = q * 8 - h;
+        if (i >= shift && i + (shift ? 16 - shift : 8) <= e.numel) {
+            float g[8], x[8], m[8], v[8];
+            const Raw<4> rm = load_raw(e.m + i, (Raw<4> *)nullptr), rv = load_raw(e.v + i, (Raw<4> *)nullptr);
+            if constexpr (MASTER)
+                to_floats(load_raw(e.master + i, (Raw<4> *)nullptr), false, x);
+            else
+                to_floats(load_raw(param + i * BP, (Raw<BP> *)nullptr), bp, x);
+            if (shift == 0)
+                to_floats(load_raw(grad + i * BG, (Raw<BG> *)nullptr), bg, g);
+            else
+                to_floats(load_shifted<BG>(grad + (i - shift) * BG, shift), bg, g);
+            to_floats(rm, false, m);
+            to_floats(rv, false, v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) step_one(s, c, decay, g[j], x[j], m[j], v[j]);
+            store_floats<4>(e.m + i, m, false);
+            store_floats<4>(e.v + i, v, false);
+            if constexpr (MASTER) store_floats<4>(e.master + i, x, false);
+            store_floats<BP>(param + i * BP, x, bp);
+        } else {
+            for (int64_t j = max(i, (int64_t)0); j < min(i + 8, e.numel); ++j)
+                step_element<BP, BG, MASTER>(e, s, c, decay, j, bp, bg);
+        }
+    }
+}
+
+template <int BP, int BG, bool MASTER, int N>
+__global__ void __launch_bounds__(kOptThreads, 4)
+adamw_kernel(const __grid_constant__ Table<ParamEntry, N> t, const __grid_constant__ Step s, bool bp, bool bg, bool chained)
+{
+    if (chained) chain();
     float c = s.scale;
     if (s.norm) {
         const float norm = *s.norm;
         if (s.skip && !isfinite(norm)) return;
         c *= clip_coef(norm, s.max_norm);
     }
-    uint32_t u = run_begin(t.units, blockIdx.x, gridDim.x);
-    const uint32_t end = run_begin(t.units, blockIdx.x + 1, gridDim.x);
-    for (int k = u < end ? entry_of(t, u) : 0; u < end; ++k) {
-        const ParamEntry &e = t.e[k];
-        const uint32_t before = k ? t.e[k - 1].unit_end : 0, stop = min(end, e.unit_end);
-        if (stop <= u) continue;
-        const int64_t i1 = min((int64_t)(stop - before) * kParamUnit, e.numel);
-        const float decay = s.lr * e.decay;
-        for (int64_t i = (int64_t)(u - before) * kParamUnit + threadIdx.x; i < i1; i += kOptThreads) {
-            const float h = load_as_float(e.grad, i, grad_type) * c;
-            const float m = fmaf(s.beta1, e.m[i], s.one_beta1 * h);
-            const float v = fmaf(s.beta2, e.v[i], s.one_beta2 * h * h);
-            float x = e.master ? e.master[i] : load_as_float(e.param, i, param_type);
-            x -= fmaf(decay, x, s.rate * (m / fmaf(sqrtf(v), s.root, s.eps)));
-            e.m[i] = m;
-            e.v[i] = v;
-            if (e.master) e.master[i] = x;
-            store_rounded(e.param, i, param_type, x);
-        }
-        u = stop;
-    }
+    const uint32_t u = gridDim.x - 1 - blockIdx.x;        // backwards: L2 still holds what the norm read last
+    const ParamEntry &e = t.e[entry_of(t, u)];
+    step_units<BP, BG, MASTER>(e, s, c, u - e.begin, u - e.begin + 1, bp, bg);
 }
 
-template <int N>
-cudaError_t launch(const ParamTable &t, Step s, int param_type, int grad_type, cudaStream_t stream)
+template <int BP, int BG, bool MASTER>
+cudaError_t launch(const ParamTable &t, Step s, bool bp, bool bg, bool chained, cudaStream_t stream)
 {
-    int64_t grid = (int64_t)sm_count() * 8;
-    if (grid > t.units) grid = t.units;
-    if (grid == 0) return cudaSuccess;
-    void *args[] = {(void *)&t, &s, &param_type, &grad_type};
-    return cudaLaunchKernel((const void *)adamw_kernel<N>, dim3((unsigned)grid), dim3(kOptThreads), args, 0, stream);
+    void *args[] = {(void *)&t, &s, &bp, &bg, &chained};
+    return launch_table(t.n <= kParamsSmall ? (const void *)adamw_kernel<BP, BG, MASTER, kParamsSmall>
+                                            : (const void *)adamw_kernel<BP, BG, MASTER, kParams>,
+                        t.units, args, chained, stream);
+}
+
+cudaError_t launch(const aspis_params::Group &g, const ParamTable &t, const Step &s, bool chained, cudaStream_t stream)
+{
+    const bool bp = g.param_type == ASPIS_BF16, bg = g.grad_type == ASPIS_BF16, wide = g.grad_type == ASPIS_F32;
+    if (g.param_type == ASPIS_F32)
+        return wide ? launch<4, 4, false>(t, s, bp, bg, chained, stream) : launch<4, 2, false>(t, s, bp, bg, chained, stream);
+    if (g.master)
+        return wide ? launch<2, 4, true>(t, s, bp, bg, chained, stream) : launch<2, 2, true>(t, s, bp, bg, chained, stream);
+    return wide ? launch<2, 4, false>(t, s, bp, bg, chained, stream) : launch<2, 2, false>(t, s, bp, bg, chained, stream);
 }
 
 }  // namespace
@@ -92,11 +152,12 @@ extern "C" aspis_status aspis_adamw(const aspis_params *params, const aspis_adam
     const cudaStream_t st = (cudaStream_t)stream;
     cudaError_t err = normed && work ? launch_grad_norm(params->grads.tables, a->scale, norm, nullptr, work, st)
                                      : cudaSuccess;
-    for (const auto &g : params->groups)
-        for (const auto &t : g.tables) {
+    bool chained = normed && work;
+    for (auto g = params->groups.rbegin(); g != params->groups.rend(); ++g)
+        for (auto t = g->tables.rbegin(); t != g->tables.rend(); ++t) {
             if (err != cudaSuccess) return ASPIS_E_CUDA;
-            err = t->n <= kParamsSmall ? launch<kParamsSmall>(*t, s, g.param_type, g.grad_type, st)
-                                       : launch<kParams>(*t, s, g.param_type, g.grad_type, st);
+            err = launch(*g, **t, s, chained, st);
+            chained = true;
         }
     return err == cudaSuccess ? ASPIS_OK : ASPIS_E_CUDA;
 }

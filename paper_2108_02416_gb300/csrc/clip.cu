@@ -1,4 +1,8 @@
 // aspis_clip_grads: the norm (norm.cu), then every gradient times s * c.
+//
+// The second kernel reads and writes eight elements per thread and access, aligned to
+// the output.  Blocks take their runs from the end of the list backwards, as what the norm
+// has read last is what L2 still holds.
 #include <math.h>
 
 #include "optim.cuh"
@@ -7,35 +11,95 @@ using namespace aspis;
 
 namespace {
 
+constexpr int kDepth = 4;         // groups of eight elements that a thread loads before it stores
+constexpr int kRun = 8;           // units per block
+
+// Units [ua, ub) of a tensor: groups of eight elements counted from the group boundary at or
+// before the output's first element.
+template <int BI, int BO>
+__device__ __forceinline__ void scale_units(const GradEntry &e, uint32_t ua, uint32_t ub, float c)
+{
+    const bool bi = e.type() == ASPIS_BF16, bo = e.out_type() == ASPIS_BF16;
+    const int64_t numel = e.numel();
+    const int h = behind<BO>(e.out);
+    const char *in = static_cast<const char *>(e.in);
+    char *out = static_cast<char *>(e.out);
+    const int shift = behind<BI>(in - h * BI);    // of the input's groups against the output's
+    constexpr int per = kOptThreads * 2 / BI;     // groups per unit
+    const int64_t end = min((int64_t)ub * per, (numel + h + 7) / 8);
+    // groups that can be taken whole: [lo, hi)
+    const int64_t lo = (h + shift + 7) / 8, hi = (numel + h - (shift ? 8 - shift : 0)) / 8;
+    for (int64_t q = (int64_t)ua * per + threadIdx.x; q < end; q += kDepth * kOptThreads) {
+        if (q >= lo && q + (kDepth - 1) * kOptThreads < min(hi, end)) {
+            Raw<BI> r[kDepth];
+#pragma unroll
+            for (int d = 0; d < kDepth; ++d) {
+                const char *p = in + ((q + d * kOptThreads) * 8 - h - shift) * BI;
+                r[d] = shift ? load_shifted<BI>(p, shift) : load_raw(p, (Raw<BI> *)nullptr);
+            }
+#pragma unroll
+            for (int d = 0; d < kDepth; ++d) {
+                float f[8];
+                to_floats(r[d], bi, f);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) f[j] *= c;
+                store_floats<BO>(out + ((q + d * kOptThreads) * 8 - h) * BO, f, bo);
+            }
+        } else {
+            for (int64_t p = q; p < min(end, q + kDepth * kOptThreads); p += kOptThreads) {
+                const int64_t i = p * 8 - h;      // the group's first element
+                if (p >= lo && p < hi) {
+                    float f[8];
+                    const char *at = in + (i - shift) * BI;
+                    to_floats(shift ? load_shifted<BI>(at, shift) : load_raw(at, (Raw<BI> *)nullptr), bi, f);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) f[j] *= c;
+                    store_floats<BO>(out + i * BO, f, bo);
+                } else {
+                    for (int64_t j = max(i, (int64_t)0); j < min(i + 8, numel); ++j)
+                        store_one<BO>(out, j, load_one<BI>(in, j, bi) * c, bo);
+                }
+            }
+        }
+    }
+}
+
 template <int N>
 __global__ void __launch_bounds__(kOptThreads)
-scale_kernel(const __grid_constant__ Table<GradEntry, N> t, float max_norm, float scale, const float *norm)
+scale_kernel(const __grid_constant__ Table<GradEntry, N> t, float max_norm, float scale, const float *norm, bool chained)
 {
-    chain();
+    if (chained) chain();
     const float c = scale * clip_coef(*norm, max_norm);
-    uint32_t u = run_begin(t.units, blockIdx.x, gridDim.x);
-    const uint32_t end = run_begin(t.units, blockIdx.x + 1, gridDim.x);
-    for (int k = u < end ? entry_of(t, u) : 0; u < end; ++k) {
+    uint32_t u = (gridDim.x - 1 - blockIdx.x) * kRun;
+    const uint32_t end = min(u + kRun, t.units);
+    for (int k = entry_of(t, u); u < end; ++k) {
         const GradEntry &e = t.e[k];
-        const uint32_t before = k ? t.e[k - 1].unit_end : 0, stop = min(end, e.unit_end);
-        if (stop <= u) continue;
-        const int unit = grad_unit(e.type);
-        const int64_t i1 = min((int64_t)(stop - before) * unit, e.numel);
-        if (c != 1.0f || e.in != e.out)
-            for (int64_t i = (int64_t)(u - before) * unit + threadIdx.x; i < i1; i += kOptThreads)
-                store_rounded(e.out, i, e.out_type, load_as_float(e.in, i, e.type) * c);
+        const uint32_t stop = min(end, e.end), ua = u - e.begin, ub = stop - e.begin;
+        if (c != 1.0f || e.in != e.out) {
+            if (e.type() == ASPIS_F32) {
+                if (e.out_type() == ASPIS_F32)
+                    scale_units<4, 4>(e, ua, ub, c);
+                else
+                    scale_units<4, 2>(e, ua, ub, c);
+            } else {
+                if (e.out_type() == ASPIS_F32)
+                    scale_units<2, 4>(e, ua, ub, c);
+                else
+                    scale_units<2, 2>(e, ua, ub, c);
+            }
+        }
         u = stop;
     }
 }
 
 template <int N>
-cudaError_t launch(const GradTable &t, float max_norm, float scale, const float *norm, cudaStream_t stream)
+cudaError_t launch(const GradTable &t, float max_norm, float scale, const float *norm, bool chained,
+                   cudaStream_t stream)
 {
-    int64_t grid = (int64_t)sm_count() * 8;
-    if (grid > t.units) grid = t.units;
+    const int64_t grid = ((int64_t)t.units + kRun - 1) / kRun;
     if (grid == 0) return cudaSuccess;
-    void *args[] = {(void *)&t, &max_norm, &scale, &norm};
-    return cudaLaunchKernel((const void *)scale_kernel<N>, dim3((unsigned)grid), dim3(kOptThreads), args, 0, stream);
+    void *args[] = {(void *)&t, &max_norm, &scale, &norm, &chained};
+    return launch_table((const void *)scale_kernel<N>, grid, args, chained, stream);
 }
 
 }  // namespace
@@ -48,11 +112,13 @@ extern "C" aspis_status aspis_clip_grads(const aspis_tensors *grads, float max_n
     if ((uintptr_t)work % 16 != 0 || (uintptr_t)norm % 4 != 0) return ASPIS_E_ALIGN;
     const cudaStream_t st = (cudaStream_t)stream;
     cudaError_t e = work ? launch_grad_norm(grads->tables, scale, norm, nullptr, work, st) : cudaSuccess;
-    for (const auto &t : grads->tables) {
-        if (e != cudaSuccess) break;
-        e = t->n <= kGradsSmall ? launch<kGradsSmall>(*t, max_norm, scale, norm, st)
-            : t->n <= kGradsMid ? launch<kGradsMid>(*t, max_norm, scale, norm, st)
-                                : launch<kGrads>(*t, max_norm, scale, norm, st);
+    bool chained = work != nullptr;
+    for (auto it = grads->tables.rbegin(); it != grads->tables.rend() && e == cudaSuccess; ++it) {
+        const GradTable &t = **it;
+        e = t.n <= kGradsSmall ? launch<kGradsSmall>(t, max_norm, scale, norm, chained, st)
+            : t.n <= kGradsMid ? launch<kGradsMid>(t, max_norm, scale, norm, chained, st)
+                               : launch<kGrads>(t, max_norm, scale, norm, chained, st);
+        chained = chained || t.units;
     }
     return e == cudaSuccess ? ASPIS_OK : ASPIS_E_CUDA;
 }

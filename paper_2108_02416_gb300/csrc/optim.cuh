@@ -19,15 +19,17 @@
 
 namespace aspis {
 
-// Work is dealt in units of consecutive elements of one tensor; a block takes a
-// contiguous run of units, found once by bisection.
+// Work is dealt in units of consecutive elements of one tensor; every tensor, an empty one
+// too, has a unit at least.
 struct GradEntry {
     const void *in;
     void *out;                    // in place: in
-    int64_t numel;
-    uint32_t unit_end;            // units of this table's tensors up to and with this one
-    uint8_t type, out_type;
-    uint16_t pad;
+    uint64_t length_types;        // elements, and the types from bit 48 and 56
+    uint32_t begin, end;          // units of the table that are this tensor's
+
+    __host__ __device__ int64_t numel() const { return (int64_t)(length_types & 0xFFFFFFFFFFFFull); }
+    __host__ __device__ int type() const { return (int)(length_types >> 48) & 0xFF; }
+    __host__ __device__ int out_type() const { return (int)(length_types >> 56); }
 };
 
 struct ParamEntry {
@@ -36,9 +38,15 @@ struct ParamEntry {
     const void *grad;
     float *m, *v;
     int64_t numel;
-    uint32_t unit_end;
+    uint32_t begin, end;
     float decay;
+    uint32_t pad;
 };
+
+// hint[u >> shift] is the tensor of the first unit with that quotient: what the constant bank
+// has to deliver before the first element can be read is the hint, its successor, few steps of a bisection
+// between them (none inside a large tensor) and the entry.
+constexpr int kHints = 64;
 
 template <class E, int N>
 struct Table {
@@ -46,35 +54,36 @@ struct Table {
     uint32_t units;
     int32_t first;                // of the list's tensors, the one that entry 0 is
     int32_t last;                 // 1: the last table of its list
+    uint32_t shift;
+    uint16_t hint[kHints + 2];
     E e[N];
 };
 
 constexpr int kGradsSmall = 120, kGradsMid = 500, kGrads = 1000;
-constexpr int kParamsSmall = 72, kParams = 576;
+constexpr int kParamsSmall = 60, kParams = 500;
 using GradTable = Table<GradEntry, kGrads>;
 using ParamTable = Table<ParamEntry, kParams>;
-static_assert(sizeof(GradTable) <= 32764 && sizeof(ParamTable) <= 32764, "a kernel argument's limit");
+static_assert(sizeof(GradTable) <= 32700 && sizeof(ParamTable) <= 32600, "a kernel's arguments have 32,764 bytes");
 
 constexpr int kOptThreads = 256;
-constexpr int kMaxGrid = 2048;    // of the norm: one partial sum per block and tensor that it meets
-static_assert(64 + 8 * (kMaxGrid + kGrads) <= ASPIS_NORM_WORKSPACE_BYTES, "workspace");
+constexpr int kMaxGrid = 1024;    // of the norm
 
 __host__ __device__ constexpr int type_bytes(int type) { return type == ASPIS_F32 ? 4 : 2; }
 // 4 KB of gradient; one vector of 16 bytes per thread
 __host__ __device__ constexpr int grad_unit(int type) { return kOptThreads * 16 / type_bytes(type); }
-constexpr int kParamUnit = 2048;
+constexpr int kParamUnit = 8 * kOptThreads;
 
 // the tensor that unit u of the table belongs to
 template <class T>
 __device__ __forceinline__ int entry_of(const T &t, uint32_t u)
 {
-    int lo = 0, hi = t.n - 1;
+    int lo = t.hint[u >> t.shift], hi = t.hint[(u >> t.shift) + 1];
     while (lo < hi) {
-        const int mid = (lo + hi) / 2;
-        if (t.e[mid].unit_end > u)
-            hi = mid;
+        const int mid = (lo + hi + 1) / 2;
+        if (t.e[mid].begin <= u)
+            lo = mid;
         else
-            lo = mid + 1;
+            hi = mid - 1;
     }
     return lo;
 }
@@ -84,21 +93,145 @@ __device__ __forceinline__ uint32_t run_begin(uint32_t units, uint32_t b, uint32
     return (uint32_t)((uint64_t)units * b / grid);
 }
 
-__device__ __forceinline__ float load_as_float(const void *p, int64_t i, int type)
+// ---- eight elements at a time: one 32-byte access of fp32, one of 16 bytes of a 16-bit type
+
+template <int B>
+struct Raw {                      // eight elements of B bytes
+    uint32_t w[2 * B];
+};
+
+// Streams are read past L1 and leave L2 first, so that gradients which the norm has just read stay there.
+__device__ __forceinline__ Raw<4> load_raw(const void *p, Raw<4> *)
 {
-    if (type == ASPIS_F32) return static_cast<const float *>(p)[i];
-    if (type == ASPIS_BF16) return __bfloat162float(static_cast<const __nv_bfloat16 *>(p)[i]);
-    return __half2float(static_cast<const __half *>(p)[i]);
+    Raw<4> r;
+    asm volatile("ld.global.L1::no_allocate.L2::evict_first.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]), "=r"(r.w[4]), "=r"(r.w[5]), "=r"(r.w[6]),
+                   "=r"(r.w[7])
+                 : "l"(p));
+    return r;
 }
 
-__device__ __forceinline__ void store_rounded(void *p, int64_t i, int type, float x)
+__device__ __forceinline__ Raw<2> load_raw(const void *p, Raw<2> *)
 {
-    if (type == ASPIS_F32)
+    const uint4 v = __ldcs(static_cast<const uint4 *>(p));
+    return Raw<2>{{v.x, v.y, v.z, v.w}};
+}
+
+__device__ __forceinline__ void store_raw(void *p, const Raw<4> &r)
+{
+    asm volatile("st.global.L1::no_allocate.L2::evict_first.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(r.w[0]),
+                 "r"(r.w[1]), "r"(r.w[2]), "r"(r.w[3]), "r"(r.w[4]), "r"(r.w[5]), "r"(r.w[6]), "r"(r.w[7])
+                 : "memory");
+}
+
+__device__ __forceinline__ void store_raw(void *p, const Raw<2> &r)
+{
+    __stcs(static_cast<uint4 *>(p), make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]));
+}
+
+// Eight elements from any element-aligned address: the two aligned groups that hold them,
+// shifted by `shift` elements (0 to 7; p is the address rounded down to a group).  The second
+// group is the next thread's first, and comes from L1.
+template <int B>
+__device__ __forceinline__ Raw<B> load_shifted(const char *p, int shift)
+{
+    constexpr int n = 2 * B;
+    uint32_t x[2 * n];
+#pragma unroll
+    for (int h = 0; h < n / 2; ++h) {
+        const uint4 v = __ldg(reinterpret_cast<const uint4 *>(p) + h);
+        x[4 * h] = v.x, x[4 * h + 1] = v.y, x[4 * h + 2] = v.z, x[4 * h + 3] = v.w;
+    }
+    constexpr int e4 = B;         // words that four elements take
+    if (shift & 4)
+#pragma unroll
+        for (int i = 0; i < 2 * n - e4; ++i) x[i] = x[i + e4];
+    if (shift & 2)
+#pragma unroll
+        for (int i = 0; i < 2 * n - e4 - e4 / 2; ++i) x[i] = x[i + e4 / 2];
+    if (shift & 1) {
+#pragma unroll
+        for (int i = 0; i < n; ++i) x[i] = B == 4 ? x[i + 1] : __funnelshift_r(x[i], x[i + 1], 16);
+    }
+    Raw<B> r;
+#pragma unroll
+    for (int i = 0; i < n; ++i) r.w[i] = x[i];
+    return r;
+}
+
+// bf16 or fp16 pair -> two floats, and back (round to nearest even)
+__device__ __forceinline__ float2 unpack(uint32_t w, bool bf16)
+{
+    if (bf16) return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+    return __half22float2(*reinterpret_cast<const __half2 *>(&w));
+}
+
+__device__ __forceinline__ uint32_t pack(float lo, float hi, bool bf16)
+{
+    uint32_t w;
+    if (bf16) {
+        const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+        w = *reinterpret_cast<const uint32_t *>(&v);
+    } else {
+        const __half2 v = __floats2half2_rn(lo, hi);
+        w = *reinterpret_cast<const uint32_t *>(&v);
+    }
+    return w;
+}
+
+__device__ __forceinline__ void to_floats(const Raw<4> &r, bool, float (&f)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(r.w[i]);
+}
+
+__device__ __forceinline__ void to_floats(const Raw<2> &r, bool bf16, float (&f)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 v = unpack(r.w[i], bf16);
+        f[2 * i] = v.x;
+        f[2 * i + 1] = v.y;
+    }
+}
+
+template <int B>
+__device__ __forceinline__ void store_floats(void *p, const float (&f)[8], bool bf16)
+{
+    Raw<B> r;
+    if constexpr (B == 4) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r.w[i] = __float_as_uint(f[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r.w[i] = pack(f[2 * i], f[2 * i + 1], bf16);
+    }
+    store_raw(p, r);
+}
+
+// one element
+template <int B>
+__device__ __forceinline__ float load_one(const void *p, int64_t i, bool bf16)
+{
+    if constexpr (B == 4) return static_cast<const float *>(p)[i];
+    const uint32_t w = static_cast<const uint16_t *>(p)[i];
+    return unpack(w, bf16).x;
+}
+
+template <int B>
+__device__ __forceinline__ void store_one(void *p, int64_t i, float x, bool bf16)
+{
+    if constexpr (B == 4)
         static_cast<float *>(p)[i] = x;
-    else if (type == ASPIS_BF16)
-        static_cast<__nv_bfloat16 *>(p)[i] = __float2bfloat16_rn(x);
     else
-        static_cast<__half *>(p)[i] = __float2half_rn(x);
+        static_cast<uint16_t *>(p)[i] = (uint16_t)(pack(x, 0.0f, bf16) & 0xFFFFu);
+}
+
+// Elements that an address lies behind the group boundary before it.
+template <int B>
+__device__ __forceinline__ int behind(const void *p)
+{
+    return (int)((uintptr_t)p % (8 * B)) / B;
 }
 
 // min(1, max_norm / (norm + eps)); NaN stays NaN
@@ -109,14 +242,19 @@ __device__ __forceinline__ float clip_coef(float norm, float max_norm)
 }
 
 // Workspace of the norm: the count of blocks that are done, the sum of the
-// tables before this one, and the partial sums.
+// tables before this one, the blocks that met each tensor, and the partial sums.
 struct NormWork {
     uint32_t done;
     uint32_t pad;
     double before;
-    double pad2[6];
-    double part[1];
+    uint16_t first[kGrads], last[kGrads];
+    double part[kMaxGrid + kGrads];
 };
+static_assert(sizeof(NormWork) <= ASPIS_NORM_WORKSPACE_BYTES, "workspace");
+
+// Launches a kernel whose first argument is a prefix of the table; chained: as a dependent of the kernel before it, which
+// belongs to the same call (chain()).
+cudaError_t launch_table(const void *kernel, int64_t grid, void **args, bool chained, cudaStream_t stream);
 
 // The norm of the list's gradients; norm (and tensor_norms) written by the last block.
 cudaError_t launch_grad_norm(const std::vector<std::unique_ptr<GradTable>> &tables, float scale, float *norm,

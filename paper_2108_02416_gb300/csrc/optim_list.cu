@@ -50,7 +50,7 @@ struct Ranges {
 };
 
 // up to 7 elements before the first aligned group shift a tensor's units
-uint32_t units_of(int64_t numel, int unit) { return numel ? (uint32_t)((numel + 7 + unit - 1) / unit) : 0; }
+uint32_t units_of(int64_t numel, int unit) { return numel ? (uint32_t)((numel + 7 + unit - 1) / unit) : 1; }
 
 // Appends tensors to tables of at most N entries (and 2^31 units).
 template <class T, class E, int N>
@@ -64,9 +64,26 @@ void append(std::vector<std::unique_ptr<T>> &tables, E e, uint32_t units, int64_
         tables.back()->last = 0;
     }
     T &t = *tables.back();
+    e.begin = t.units;
     t.units += units;
-    e.unit_end = t.units;
+    e.end = t.units;
     t.e[t.n++] = e;
+}
+
+template <class T>
+void finish(std::vector<std::unique_ptr<T>> &tables)
+{
+    for (auto &p : tables) {
+        T &t = *p;
+        t.last = &p == &tables.back();
+        t.shift = 0;
+        while (t.units > 0 && (t.units - 1) >> t.shift >= kHints) ++t.shift;
+        int k = 0;
+        for (uint32_t j = 0; j < kHints + 2; ++j) {
+            while (k + 1 < t.n && t.e[k].end <= (uint64_t)j << t.shift) ++k;
+            t.hint[j] = (uint16_t)k;
+        }
+    }
 }
 
 void add_grad(aspis_tensors &list, const void *in, void *out, int64_t numel, int type, int out_type)
@@ -74,22 +91,15 @@ void add_grad(aspis_tensors &list, const void *in, void *out, int64_t numel, int
     GradEntry e = {};
     e.in = in;
     e.out = out;
-    e.numel = numel;
-    e.type = (uint8_t)type;
-    e.out_type = (uint8_t)out_type;
+    e.length_types = (uint64_t)numel | (uint64_t)type << 48 | (uint64_t)out_type << 56;
     append<GradTable, GradEntry, kGrads>(list.tables, e, units_of(numel, grad_unit(type)), list.n);
     ++list.n;
 }
 
 void finish(aspis_tensors &list)
 {
-    if (list.tables.empty()) {
-        list.tables.push_back(std::make_unique<GradTable>());
-        list.tables.back()->n = 0;
-        list.tables.back()->units = 0;
-        list.tables.back()->first = 0;
-    }
-    list.tables.back()->last = 1;
+    if (list.tables.empty()) list.tables.push_back(std::make_unique<GradTable>());      // an empty list's norm is 0
+    finish(list.tables);
 }
 
 aspis_status make_tensors(const aspis_tensor *t, int64_t n, aspis_tensors &list)
@@ -153,6 +163,7 @@ aspis_status make_params(const aspis_param *p, int64_t n, aspis_params &list)
         e.decay = x.weight_decay;
         append<ParamTable, ParamEntry, kParams>(g->tables, e, units_of(x.numel, kParamUnit), i);
     }
+    for (auto &g : list.groups) finish(g.tables);
     return ASPIS_OK;
 }
 
