@@ -41,7 +41,7 @@
 extern "C" {
 #endif
 
-#define ASPIS_NORM_WORKSPACE_BYTES 32768
+#define ASPIS_NORM_WORKSPACE_BYTES 40960
 #define ASPIS_CLIP_EPS 1e-6f          /* added to the norm in the clipping quotient */
 
 typedef enum { ASPIS_F32 = 0, ASPIS_BF16 = 1, ASPIS_F16 = 2 } aspis_dtype;

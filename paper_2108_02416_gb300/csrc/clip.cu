@@ -11,8 +11,9 @@ using namespace aspis;
 
 namespace {
 
-constexpr int kDepth = 4;         // groups of eight elements that a thread loads before it stores
-constexpr int kRun = 8;           // units per block
+constexpr int kDepth = 2;         // groups of eight elements that a thread loads before it stores
+constexpr int kRun = 8;           // units that a block takes at a time
+constexpr int kBlocks = 8;        // per multiprocessor
 
 // Units [ua, ub) of a tensor: groups of eight elements counted from the group boundary at or
 // before the output's first element.
@@ -65,30 +66,34 @@ __device__ __forceinline__ void scale_units(const GradEntry &e, uint32_t ua, uin
 }
 
 template <int N>
-__global__ void __launch_bounds__(kOptThreads)
+__global__ void __launch_bounds__(kOptThreads, 6)
 scale_kernel(const __grid_constant__ Table<GradEntry, N> t, float max_norm, float scale, const float *norm, bool chained)
 {
     if (chained) chain();
     const float c = scale * clip_coef(*norm, max_norm);
-    uint32_t u = (gridDim.x - 1 - blockIdx.x) * kRun;
-    const uint32_t end = min(u + kRun, t.units);
-    for (int k = entry_of(t, u); u < end; ++k) {
-        const GradEntry &e = t.e[k];
-        const uint32_t stop = min(end, e.end), ua = u - e.begin, ub = stop - e.begin;
-        if (c != 1.0f || e.in != e.out) {
-            if (e.type() == ASPIS_F32) {
-                if (e.out_type() == ASPIS_F32)
-                    scale_units<4, 4>(e, ua, ub, c);
-                else
-                    scale_units<4, 2>(e, ua, ub, c);
-            } else {
-                if (e.out_type() == ASPIS_F32)
-                    scale_units<2, 4>(e, ua, ub, c);
-                else
-                    scale_units<2, 2>(e, ua, ub, c);
+    if (c == 1.0f && t.in_place) return;
+    const uint32_t runs = (t.units + kRun - 1) / kRun;
+    for (uint32_t r = blockIdx.x; r < runs; r += gridDim.x) {
+        uint32_t u = (runs - 1 - r) * kRun;
+        const uint32_t end = min(u + kRun, t.units);
+        for (int k = entry_of(t, u); u < end; ++k) {
+            const GradEntry &e = t.e[k];
+            const uint32_t stop = min(end, e.end), ua = u - e.begin, ub = stop - e.begin;
+            if (c != 1.0f || e.in != e.out) {
+                if (e.type() == ASPIS_F32) {
+                    if (e.out_type() == ASPIS_F32)
+                        scale_units<4, 4>(e, ua, ub, c);
+                    else
+                        scale_units<4, 2>(e, ua, ub, c);
+                } else {
+                    if (e.out_type() == ASPIS_F32)
+                        scale_units<2, 4>(e, ua, ub, c);
+                    else
+                        scale_units<2, 2>(e, ua, ub, c);
+                }
             }
+            u = stop;
         }
-        u = stop;
     }
 }
 
@@ -96,7 +101,9 @@ template <int N>
 cudaError_t launch(const GradTable &t, float max_norm, float scale, const float *norm, bool chained,
                    cudaStream_t stream)
 {
-    const int64_t grid = ((int64_t)t.units + kRun - 1) / kRun;
+    const int64_t runs = ((int64_t)t.units + kRun - 1) / kRun;
+    const int64_t most = t.in_place ? (int64_t)sm_count() * kBlocks : runs;
+    const int64_t grid = runs < most ? runs : most;
     if (grid == 0) return cudaSuccess;
     void *args[] = {(void *)&t, &max_norm, &scale, &norm, &chained};
     return launch_table((const void *)scale_kernel<N>, grid, args, chained, stream);

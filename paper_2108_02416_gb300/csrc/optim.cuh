@@ -55,6 +55,7 @@ struct Table {
     int32_t first;                // of the list's tensors, the one that entry 0 is
     int32_t last;                 // 1: the last table of its list
     uint32_t shift;
+    int32_t in_place;             // 1: every tensor is clipped in place
     uint16_t hint[kHints + 2];
     E e[N];
 };
@@ -248,7 +249,8 @@ struct NormWork {
     uint32_t pad;
     double before;
     uint16_t first[kGrads], last[kGrads];
-    double part[kMaxGrid + kGrads];
+    float2 pair[kMaxGrid + kGrads];
+    double wide[kMaxGrid + kGrads];
 };
 static_assert(sizeof(NormWork) <= ASPIS_NORM_WORKSPACE_BYTES, "workspace");
 

@@ -100,6 +100,8 @@ void finish(aspis_tensors &list)
 {
     if (list.tables.empty()) list.tables.push_back(std::make_unique<GradTable>());      // an empty list's norm is 0
     finish(list.tables);
+    for (auto &t : list.tables)
+        t->in_place = std::all_of(t->e, t->e + t->n, [](const GradEntry &e) { return e.in == e.out; });
 }
 
 aspis_status make_tensors(const aspis_tensor *t, int64_t n, aspis_tensors &list)
