@@ -1,13 +1,20 @@
 // aspis_adamw: the norm (norm.cu), then one AdamW step on every tensor with the
 // gradient read through the clipping coefficient.  The step streams every array once, eight
 // elements per thread and access, and is bound by HBM.
-#include <math.h>
-
-#include "optim.cuh"
+#include "norm.cuh"
 
 using namespace aspis;
 
 namespace {
+
+constexpr int kTogether = 3;      // blocks of the cooperative kernel per multiprocessor
+constexpr int64_t kMostTogether = 2000;           // units
+
+template <int P, int G, bool M>
+struct Types {
+    static constexpr int param = P, grad = G;
+    static constexpr bool master = M;
+};
 
 struct Step {
     float beta1, one_beta1, beta2, one_beta2;
@@ -105,6 +112,56 @@ adamw_kernel(const __grid_constant__ Table<ParamEntry, N> t, const __grid_consta
     step_units<BP, BG, MASTER>(e, s, c, u - e.begin, u - e.begin + 1, bp, bg);
 }
 
+__device__ __forceinline__ void prefetch(const void *p)
+{
+    asm volatile("prefetch.global.L2 [%0];" ::"l"(p));
+}
+
+// Norm and step in one cooperative kernel: every block sums the gradients of a run of units, waits
+// for the others, and steps the same run, whose first state it has called into L2 meanwhile.
+template <int BP, int BG, bool MASTER, int N>
+__global__ void __launch_bounds__(kOptThreads, kTogether)
+clipped_adamw_kernel(const __grid_constant__ Table<ParamEntry, N> t, const __grid_constant__ Step s, bool bp, bool bg,
+                     float *norm, NormWork *work)
+{
+    const uint32_t begin = run_begin(t.units, blockIdx.x, gridDim.x), end = run_begin(t.units, blockIdx.x + 1, gridDim.x);
+    const int first = entry_of(t, begin);
+    {
+        const ParamEntry &e = t.e[first];
+        const int64_t i = (int64_t)(begin - e.begin) * kParamUnit + 8 * threadIdx.x;
+        if (i < e.numel) {
+            prefetch(e.m + i);
+            prefetch(e.v + i);
+            if (MASTER)
+                prefetch(e.master + i);
+            else
+                prefetch(static_cast<const char *>(e.param) + i * BP);
+        }
+    }
+    Sum sum;
+    uint32_t u = begin;
+    for (int k = first; u < end; ++k) {
+        const ParamEntry &e = t.e[k];
+        const uint32_t stop = min(end, e.end);
+        constexpr uint32_t per = kParamUnit / grad_unit(BG == 4 ? ASPIS_F32 : ASPIS_BF16);
+        sum_units(sum, e.grad, e.numel, BG == 4 ? ASPIS_F32 : bg ? ASPIS_BF16 : ASPIS_F16, (u - e.begin) * per,
+                  (stop - e.begin) * per);
+        u = stop;
+    }
+    float all;
+    const bool met = meet(sum, s.scale, work, all);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *norm = all;
+    if (!met || (s.skip && !isfinite(all))) return;
+    const float c = s.scale * clip_coef(all, s.max_norm);
+    u = begin;
+    for (int k = first; u < end; ++k) {
+        const ParamEntry &e = t.e[k];
+        const uint32_t stop = min(end, e.end);
+        step_units<BP, BG, MASTER>(e, s, c, u - e.begin, stop - e.begin, bp, bg);
+        u = stop;
+    }
+}
+
 template <int BP, int BG, bool MASTER>
 cudaError_t launch(const ParamTable &t, Step s, bool bp, bool bg, bool chained, cudaStream_t stream)
 {
@@ -114,14 +171,26 @@ cudaError_t launch(const ParamTable &t, Step s, bool bp, bool bg, bool chained, 
                         t.units, args, chained, stream);
 }
 
-cudaError_t launch(const aspis_params::Group &g, const ParamTable &t, const Step &s, bool chained, cudaStream_t stream)
+template <int BP, int BG, bool MASTER>
+bool launch_clipped(cudaError_t &err, const ParamTable &t, Step s, bool bp, bool bg, float *norm, void *work,
+                    cudaStream_t stream)
 {
-    const bool bp = g.param_type == ASPIS_BF16, bg = g.grad_type == ASPIS_BF16, wide = g.grad_type == ASPIS_F32;
-    if (g.param_type == ASPIS_F32)
-        return wide ? launch<4, 4, false>(t, s, bp, bg, chained, stream) : launch<4, 2, false>(t, s, bp, bg, chained, stream);
-    if (g.master)
-        return wide ? launch<2, 4, true>(t, s, bp, bg, chained, stream) : launch<2, 2, true>(t, s, bp, bg, chained, stream);
-    return wide ? launch<2, 4, false>(t, s, bp, bg, chained, stream) : launch<2, 2, false>(t, s, bp, bg, chained, stream);
+    const int64_t most = (int64_t)sm_count() * kTogether;
+    void *args[] = {(void *)&t, &s, &bp, &bg, &norm, &work};
+    return launch_together(err,
+                           t.n <= kParamsSmall ? (const void *)clipped_adamw_kernel<BP, BG, MASTER, kParamsSmall>
+                                               : (const void *)clipped_adamw_kernel<BP, BG, MASTER, kParams>,
+                           t.units < most ? t.units : most, args, stream);
+}
+
+// calls f with the sizes of a group's types as template arguments
+template <class F>
+auto by_types(const aspis_params::Group &g, F f)
+{
+    const bool wide = g.grad_type == ASPIS_F32;
+    if (g.param_type == ASPIS_F32) return wide ? f(Types<4, 4, false>()) : f(Types<4, 2, false>());
+    if (g.master) return wide ? f(Types<2, 4, true>()) : f(Types<2, 2, true>());
+    return wide ? f(Types<2, 4, false>()) : f(Types<2, 2, false>());
 }
 
 }  // namespace
@@ -150,13 +219,26 @@ extern "C" aspis_status aspis_adamw(const aspis_params *params, const aspis_adam
     s.norm = normed ? norm : nullptr;
     s.skip = a->skip_nonfinite;
     const cudaStream_t st = (cudaStream_t)stream;
-    cudaError_t err = normed && work ? launch_grad_norm(params->grads.tables, a->scale, norm, nullptr, work, st)
+    cudaError_t err = cudaSuccess;
+    if (normed && work && params->groups.size() == 1 && params->groups[0].tables.size() == 1 &&
+        params->groups[0].tables[0]->units <= kMostTogether) {
+        const auto &g = params->groups[0];
+        if (by_types(g, [&](auto k) {
+                return launch_clipped<k.param, k.grad, k.master>(err, *g.tables[0], s, g.param_type == ASPIS_BF16,
+                                                                 g.grad_type == ASPIS_BF16, norm, work, st);
+            }))
+            return err == cudaSuccess ? ASPIS_OK : ASPIS_E_CUDA;
+    }
+    err = normed && work ? launch_grad_norm(params->grads.tables, a->scale, norm, nullptr, work, st)
                                      : cudaSuccess;
     bool chained = normed && work;
     for (auto g = params->groups.rbegin(); g != params->groups.rend(); ++g)
         for (auto t = g->tables.rbegin(); t != g->tables.rend(); ++t) {
             if (err != cudaSuccess) return ASPIS_E_CUDA;
-            err = launch(*g, **t, s, chained, st);
+            err = by_types(*g, [&](auto k) {
+                return launch<k.param, k.grad, k.master>(**t, s, g->param_type == ASPIS_BF16, g->grad_type == ASPIS_BF16,
+                                                         chained, st);
+            });
             chained = true;
         }
     return err == cudaSuccess ? ASPIS_OK : ASPIS_E_CUDA;

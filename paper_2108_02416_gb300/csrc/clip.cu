@@ -3,9 +3,7 @@
 // The second kernel reads and writes eight elements per thread and access, aligned to
 // the output.  Blocks take their runs from the end of the list backwards, as what the norm
 // has read last is what L2 still holds.
-#include <math.h>
-
-#include "optim.cuh"
+#include "norm.cuh"
 
 using namespace aspis;
 
@@ -14,6 +12,8 @@ namespace {
 constexpr int kDepth = 2;         // groups of eight elements that a thread loads before it stores
 constexpr int kRun = 8;           // units that a block takes at a time
 constexpr int kBlocks = 8;        // per multiprocessor
+constexpr int kTogether = 3;      // blocks of the cooperative kernel per multiprocessor
+constexpr int64_t kMostTogether = 16384;          // units
 
 // Units [ua, ub) of a tensor: groups of eight elements counted from the group boundary at or
 // before the output's first element.
@@ -65,6 +65,22 @@ __device__ __forceinline__ void scale_units(const GradEntry &e, uint32_t ua, uin
     }
 }
 
+__device__ __forceinline__ void scale_units(const GradEntry &e, uint32_t ua, uint32_t ub, float c)
+{
+    if (c == 1.0f && e.in == e.out) return;
+    if (e.type() == ASPIS_F32) {
+        if (e.out_type() == ASPIS_F32)
+            scale_units<4, 4>(e, ua, ub, c);
+        else
+            scale_units<4, 2>(e, ua, ub, c);
+    } else {
+        if (e.out_type() == ASPIS_F32)
+            scale_units<2, 4>(e, ua, ub, c);
+        else
+            scale_units<2, 2>(e, ua, ub, c);
+    }
+}
+
 template <int N>
 __global__ void __launch_bounds__(kOptThreads, 6)
 scale_kernel(const __grid_constant__ Table<GradEntry, N> t, float max_norm, float scale, const float *norm, bool chained)
@@ -78,22 +94,40 @@ scale_kernel(const __grid_constant__ Table<GradEntry, N> t, float max_norm, floa
         const uint32_t end = min(u + kRun, t.units);
         for (int k = entry_of(t, u); u < end; ++k) {
             const GradEntry &e = t.e[k];
-            const uint32_t stop = min(end, e.end), ua = u - e.begin, ub = stop - e.begin;
-            if (c != 1.0f || e.in != e.out) {
-                if (e.type() == ASPIS_F32) {
-                    if (e.out_type() == ASPIS_F32)
-                        scale_units<4, 4>(e, ua, ub, c);
-                    else
-                        scale_units<4, 2>(e, ua, ub, c);
-                } else {
-                    if (e.out_type() == ASPIS_F32)
-                        scale_units<2, 4>(e, ua, ub, c);
-                    else
-                        scale_units<2, 2>(e, ua, ub, c);
-                }
-            }
+            const uint32_t stop = min(end, e.end);
+            scale_units(e, u - e.begin, stop - e.begin, c);
             u = stop;
         }
+    }
+}
+
+// Norm and clipping in one cooperative kernel: every block sums a run of units, waits for the others, and
+// scales the same run.
+template <int N>
+__global__ void __launch_bounds__(kOptThreads, kTogether)
+clip_kernel(const __grid_constant__ Table<GradEntry, N> t, float max_norm, float scale, float *norm, NormWork *work)
+{
+    const uint32_t begin = run_begin(t.units, blockIdx.x, gridDim.x), end = run_begin(t.units, blockIdx.x + 1, gridDim.x);
+    const int first = entry_of(t, begin);
+    Sum sum;
+    uint32_t u = begin;
+    for (int k = first; u < end; ++k) {
+        const GradEntry &e = t.e[k];
+        const uint32_t stop = min(end, e.end);
+        sum_units(sum, e.in, e.numel(), e.type(), u - e.begin, stop - e.begin);
+        u = stop;
+    }
+    float all;
+    const bool met = meet(sum, scale, work, all);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *norm = all;
+    if (!met) return;
+    const float c = scale * clip_coef(all, max_norm);
+    u = begin;
+    for (int k = first; u < end; ++k) {
+        const GradEntry &e = t.e[k];
+        const uint32_t stop = min(end, e.end);
+        scale_units(e, u - e.begin, stop - e.begin, c);
+        u = stop;
     }
 }
 
@@ -109,6 +143,15 @@ cudaError_t launch(const GradTable &t, float max_norm, float scale, const float 
     return launch_table((const void *)scale_kernel<N>, grid, args, chained, stream);
 }
 
+template <int N>
+bool launch_clip(cudaError_t &err, const GradTable &t, float max_norm, float scale, float *norm, void *work,
+                 cudaStream_t stream)
+{
+    const int64_t most = (int64_t)sm_count() * kTogether;
+    void *args[] = {(void *)&t, &max_norm, &scale, &norm, &work};
+    return launch_together(err, (const void *)clip_kernel<N>, t.units < most ? t.units : most, args, stream);
+}
+
 }  // namespace
 
 extern "C" aspis_status aspis_clip_grads(const aspis_tensors *grads, float max_norm, float scale, float *norm,
@@ -118,7 +161,14 @@ extern "C" aspis_status aspis_clip_grads(const aspis_tensors *grads, float max_n
         return ASPIS_E_INVAL;
     if ((uintptr_t)work % 16 != 0 || (uintptr_t)norm % 4 != 0) return ASPIS_E_ALIGN;
     const cudaStream_t st = (cudaStream_t)stream;
-    cudaError_t e = work ? launch_grad_norm(grads->tables, scale, norm, nullptr, work, st) : cudaSuccess;
+    cudaError_t e = cudaSuccess;
+    if (const GradTable &t = *grads->tables[0]; work && t.last && t.units > 0 && t.units <= kMostTogether) {
+        if (t.n <= kGradsSmall ? launch_clip<kGradsSmall>(e, t, max_norm, scale, norm, work, st)
+            : t.n <= kGradsMid ? launch_clip<kGradsMid>(e, t, max_norm, scale, norm, work, st)
+                               : launch_clip<kGrads>(e, t, max_norm, scale, norm, work, st))
+            return e == cudaSuccess ? ASPIS_OK : ASPIS_E_CUDA;
+    }
+    e = work ? launch_grad_norm(grads->tables, scale, norm, nullptr, work, st) : cudaSuccess;
     bool chained = work != nullptr;
     for (auto it = grads->tables.rbegin(); it != grads->tables.rend() && e == cudaSuccess; ++it) {
         const GradTable &t = **it;

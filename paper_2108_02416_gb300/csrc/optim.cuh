@@ -242,21 +242,25 @@ __device__ __forceinline__ float clip_coef(float norm, float max_norm)
     return c > 1.0f ? 1.0f : c;
 }
 
-// Workspace of the norm: the count of blocks that are done, the sum of the
-// tables before this one, the blocks that met each tensor, and the partial sums.
+// Workspace of the norm: the counts of blocks that are done and that have seen the others done, the sum of
+// the tables before this one, the blocks that met each tensor, and the partial sums.
 struct NormWork {
-    uint32_t done;
-    uint32_t pad;
+    uint32_t done, left;
     double before;
     uint16_t first[kGrads], last[kGrads];
     float2 pair[kMaxGrid + kGrads];
     double wide[kMaxGrid + kGrads];
 };
+static_assert(offsetof(NormWork, first) % 16 == 0 && offsetof(NormWork, last) % 16 == 0 &&
+                  offsetof(NormWork, pair) % 16 == 0 && kGrads % 8 == 0, "fetched in steps of 16 bytes");
 static_assert(sizeof(NormWork) <= ASPIS_NORM_WORKSPACE_BYTES, "workspace");
 
 // Launches a kernel whose first argument is a prefix of the table; chained: as a dependent of the kernel before it, which
 // belongs to the same call (chain()).
 cudaError_t launch_table(const void *kernel, int64_t grid, void **args, bool chained, cudaStream_t stream);
+
+// The same as a cooperative kernel; false (and nothing enqueued) where its blocks do not fit the device at once.
+bool launch_together(cudaError_t &err, const void *kernel, int64_t grid, void **args, cudaStream_t stream);
 
 // The norm of the list's gradients; norm (and tensor_norms) written by the last block.
 cudaError_t launch_grad_norm(const std::vector<std::unique_ptr<GradTable>> &tables, float scale, float *norm,
