@@ -60,7 +60,7 @@ typedef struct aspis_tensors aspis_tensors;
 /* Checks n tensors and makes a list of them in *out.  Host only.
  * ASPIS_E_INVAL: a NULL pointer, a negative length or count, an unknown type;
  * ASPIS_E_ALIGN: an address that is no multiple of its element's size;
- * ASPIS_E_RANGE: more than 2^40 elements in a tensor, more than 2^24 tensors, or no
+ * ASPIS_E_RANGE: more than 2^38 elements in a tensor, more than 2^24 tensors, or no
  * memory for the list.
  * Tensors may overlap for the norm; aspis_clip_grads refuses a list in which a
  * range that it writes overlaps another range (out may be data itself). */

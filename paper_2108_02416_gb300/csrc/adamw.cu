@@ -8,7 +8,7 @@ using namespace aspis;
 namespace {
 
 constexpr int kTogether = 3;      // blocks of the cooperative kernel per multiprocessor
-constexpr int64_t kMostTogether = 2000;           // units
+constexpr int64_t kMostTogether = 2560;           // units
 
 template <int P, int G, bool M>
 struct Types {
@@ -48,51 +48,47 @@ __device__ __forceinline__ void step_element(const ParamEntry &e, const Step &s,
     store_one<BP>(e.param, i, x, bp);
 }
 
-// Units [ua, ub) of a tensor: groups of eight elements, one per thread, counted from the group
+// A warp's unit of a tensor: groups of eight elements, one per thread, counted from the group
 // boundary at or before the first moment's first element.  The gradient may lie behind that boundary by
 // any number of elements (a view of a flat aggregate); arrays that are written and do not share
 // it are taken element by element.
 template <int BP, int BG, bool MASTER>
-__device__ __forceinline__ void step_units(const ParamEntry &e, const Step &s, float c, uint32_t ua, uint32_t ub, bool bp,
-                                           bool bg)
+__device__ __forceinline__ void step_unit(const ParamEntry &e, const Step &s, float c, uint32_t unit, bool bp, bool bg)
 {
     const float decay = s.lr * e.decay;
-    const int h = behind<4>(e.m);
-    const int64_t first = (int64_t)ua * kParamUnit, last = (int64_t)ub * kParamUnit;
+    const int lane = threadIdx.x % 32, h = behind<4>(e.m);
+    const int64_t first = (int64_t)unit * kParamUnit;
     if (behind<4>(e.v) != h || behind<BP>(e.param) != h || (MASTER && behind<4>(e.master) != h)) {
-        for (int64_t i = first + threadIdx.x; i < min(last, e.numel); i += kOptThreads)
+        for (int64_t i = first + lane; i < min(first + kParamUnit, e.numel); i += 32)
             step_element<BP, BG, MASTER>(e, s, c, decay, i, bp, bg);
         return;
     }
     const char *grad = static_cast<const char *>(e.grad);
     char *param = static_cast<char *>(e.param);
     const int shift = behind<BG>(grad - h * BG);
-    const int64_t end = min(last / 8, (e.numel + h + 7) / 8);
-    for (int64_t q = first / 8 + threadIdx.x; q < end; q += kOptThreads) {
-        const int64_t i = q * 8 - h;
-        if (i >= shift && i + (shift ? 16 - shift : 8) <= e.numel) {
-            float g[8], x[8], m[8], v[8];
-            const Raw<4> rm = load_raw(e.m + i, (Raw<4> *)nullptr), rv = load_raw(e.v + i, (Raw<4> *)nullptr);
-            if constexpr (MASTER)
-                to_floats(load_raw(e.master + i, (Raw<4> *)nullptr), false, x);
-            else
-                to_floats(load_raw(param + i * BP, (Raw<BP> *)nullptr), bp, x);
-            if (shift == 0)
-                to_floats(load_raw(grad + i * BG, (Raw<BG> *)nullptr), bg, g);
-            else
-                to_floats(load_shifted<BG>(grad + (i - shift) * BG, shift), bg, g);
-            to_floats(rm, false, m);
-            to_floats(rv, false, v);
+    const int64_t i = first + 8 * lane - h;       // the group's first element
+    if (i >= shift && i + (shift ? 16 - shift : 8) <= e.numel) {
+        float g[8], x[8], m[8], v[8];
+        const Raw<4> rm = load_raw(e.m + i, (Raw<4> *)nullptr), rv = load_raw(e.v + i, (Raw<4> *)nullptr);
+        if constexpr (MASTER)
+            to_floats(load_raw(e.master + i, (Raw<4> *)nullptr), false, x);
+        else
+            to_floats(load_raw(param + i * BP, (Raw<BP> *)nullptr), bp, x);
+        if (shift == 0)
+            to_floats(load_raw(grad + i * BG, (Raw<BG> *)nullptr), bg, g);
+        else
+            to_floats(load_shifted<BG>(grad + (i - shift) * BG, shift), bg, g);
+        to_floats(rm, false, m);
+        to_floats(rv, false, v);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) step_one(s, c, decay, g[j], x[j], m[j], v[j]);
-            store_floats<4>(e.m + i, m, false);
-            store_floats<4>(e.v + i, v, false);
-            if constexpr (MASTER) store_floats<4>(e.master + i, x, false);
-            store_floats<BP>(param + i * BP, x, bp);
-        } else {
-            for (int64_t j = max(i, (int64_t)0); j < min(i + 8, e.numel); ++j)
-                step_element<BP, BG, MASTER>(e, s, c, decay, j, bp, bg);
-        }
+        for (int j = 0; j < 8; ++j) step_one(s, c, decay, g[j], x[j], m[j], v[j]);
+        store_floats<4>(e.m + i, m, false);
+        store_floats<4>(e.v + i, v, false);
+        if constexpr (MASTER) store_floats<4>(e.master + i, x, false);
+        store_floats<BP>(param + i * BP, x, bp);
+    } else {
+        for (int64_t j = max(i, (int64_t)0); j < min(i + 8, e.numel); ++j)
+            step_element<BP, BG, MASTER>(e, s, c, decay, j, bp, bg);
     }
 }
 
@@ -107,9 +103,11 @@ adamw_kernel(const __grid_constant__ Table<ParamEntry, N> t, const __grid_consta
         if (s.skip && !isfinite(norm)) return;
         c *= clip_coef(norm, s.max_norm);
     }
-    const uint32_t u = gridDim.x - 1 - blockIdx.x;        // backwards: L2 still holds what the norm read last
+    // from the end backwards: L2 still holds what the norm read last
+    const uint32_t u = (gridDim.x - 1 - blockIdx.x) * kWarps + threadIdx.x / 32;
+    if (u >= t.units) return;
     const ParamEntry &e = t.e[entry_of(t, u)];
-    step_units<BP, BG, MASTER>(e, s, c, u - e.begin, u - e.begin + 1, bp, bg);
+    step_unit<BP, BG, MASTER>(e, s, c, u - e.begin, bp, bg);
 }
 
 __device__ __forceinline__ void prefetch(const void *p)
@@ -124,41 +122,35 @@ __global__ void __launch_bounds__(kOptThreads, kTogether)
 clipped_adamw_kernel(const __grid_constant__ Table<ParamEntry, N> t, const __grid_constant__ Step s, bool bp, bool bg,
                      float *norm, NormWork *work)
 {
-    const uint32_t begin = run_begin(t.units, blockIdx.x, gridDim.x), end = run_begin(t.units, blockIdx.x + 1, gridDim.x);
-    const int first = entry_of(t, begin);
-    {
-        const ParamEntry &e = t.e[first];
-        const int64_t i = (int64_t)(begin - e.begin) * kParamUnit + 8 * threadIdx.x;
-        if (i < e.numel) {
-            prefetch(e.m + i);
-            prefetch(e.v + i);
-            if (MASTER)
-                prefetch(e.master + i);
-            else
-                prefetch(static_cast<const char *>(e.param) + i * BP);
-        }
-    }
+    const uint32_t begin = run_begin(t.units, blockIdx.x, gridDim.x) + threadIdx.x / 32;
+    const uint32_t end = run_begin(t.units, blockIdx.x + 1, gridDim.x);
     Sum sum;
-    uint32_t u = begin;
-    for (int k = first; u < end; ++k) {
-        const ParamEntry &e = t.e[k];
-        const uint32_t stop = min(end, e.end);
-        constexpr uint32_t per = kParamUnit / grad_unit(BG == 4 ? ASPIS_F32 : ASPIS_BF16);
-        sum_units(sum, e.grad, e.numel, BG == 4 ? ASPIS_F32 : bg ? ASPIS_BF16 : ASPIS_F16, (u - e.begin) * per,
-                  (stop - e.begin) * per);
-        u = stop;
+    for (uint32_t u = begin; u < end; u += kWarps) {
+        const ParamEntry &e = t.e[entry_of(t, u)];
+        if (u == begin) {
+            const int64_t i = (int64_t)(u - e.begin) * kParamUnit + 8 * (threadIdx.x % 32);
+            if (i < e.numel) {
+                prefetch(e.m + i);
+                prefetch(e.v + i);
+                if (MASTER)
+                    prefetch(e.master + i);
+                else
+                    prefetch(static_cast<const char *>(e.param) + i * BP);
+            }
+        }
+        constexpr int vecs = kParamUnit * BG / 16;
+        const int64_t a = (int64_t)(u - e.begin) * vecs;
+        sum_range<32>(sum, e.grad, e.numel, BG == 4 ? ASPIS_F32 : bg ? ASPIS_BF16 : ASPIS_F16, a, a + vecs,
+                      threadIdx.x % 32);
     }
     float all;
     const bool met = meet(sum, s.scale, work, all);
     if (blockIdx.x == 0 && threadIdx.x == 0) *norm = all;
     if (!met || (s.skip && !isfinite(all))) return;
     const float c = s.scale * clip_coef(all, s.max_norm);
-    u = begin;
-    for (int k = first; u < end; ++k) {
-        const ParamEntry &e = t.e[k];
-        const uint32_t stop = min(end, e.end);
-        step_units<BP, BG, MASTER>(e, s, c, u - e.begin, stop - e.begin, bp, bg);
-        u = stop;
+    for (uint32_t u = begin; u < end; u += kWarps) {
+        const ParamEntry &e = t.e[entry_of(t, u)];
+        step_unit<BP, BG, MASTER>(e, s, c, u - e.begin, bp, bg);
     }
 }
 
@@ -168,19 +160,19 @@ cudaError_t launch(const ParamTable &t, Step s, bool bp, bool bg, bool chained, 
     void *args[] = {(void *)&t, &s, &bp, &bg, &chained};
     return launch_table(t.n <= kParamsSmall ? (const void *)adamw_kernel<BP, BG, MASTER, kParamsSmall>
                                             : (const void *)adamw_kernel<BP, BG, MASTER, kParams>,
-                        t.units, args, chained, stream);
+                        ((int64_t)t.units + kWarps - 1) / kWarps, args, chained, stream);
 }
 
 template <int BP, int BG, bool MASTER>
 bool launch_clipped(cudaError_t &err, const ParamTable &t, Step s, bool bp, bool bg, float *norm, void *work,
                     cudaStream_t stream)
 {
-    const int64_t most = (int64_t)sm_count() * kTogether;
+    const int64_t all = ((int64_t)t.units + kWarps - 1) / kWarps, most = (int64_t)sm_count() * kTogether;
     void *args[] = {(void *)&t, &s, &bp, &bg, &norm, &work};
     return launch_together(err,
                            t.n <= kParamsSmall ? (const void *)clipped_adamw_kernel<BP, BG, MASTER, kParamsSmall>
                                                : (const void *)clipped_adamw_kernel<BP, BG, MASTER, kParams>,
-                           t.units < most ? t.units : most, args, stream);
+                           all < most ? all : most, args, stream);
 }
 
 // calls f with the sizes of a group's types as template arguments

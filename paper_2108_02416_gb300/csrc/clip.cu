@@ -9,16 +9,15 @@ using namespace aspis;
 
 namespace {
 
-constexpr int kDepth = 2;         // groups of eight elements that a thread loads before it stores
-constexpr int kRun = 8;           // units that a block takes at a time
-constexpr int kBlocks = 8;        // per multiprocessor
+constexpr int kDepthBytes = 128;  // that a thread loads before it stores
+constexpr int kBlocks = 8;        // per multiprocessor, where the call may turn out to write nothing
 constexpr int kTogether = 3;      // blocks of the cooperative kernel per multiprocessor
 constexpr int64_t kMostTogether = 16384;          // units
 
-// Units [ua, ub) of a tensor: groups of eight elements counted from the group boundary at or
-// before the output's first element.
+// A warp's unit of a tensor: groups of eight elements counted from the group boundary at or before
+// the output's first element.
 template <int BI, int BO>
-__device__ __forceinline__ void scale_units(const GradEntry &e, uint32_t ua, uint32_t ub, float c)
+__device__ __forceinline__ void scale_unit(const GradEntry &e, uint32_t unit, float c)
 {
     const bool bi = e.type() == ASPIS_BF16, bo = e.out_type() == ASPIS_BF16;
     const int64_t numel = e.numel();
@@ -26,28 +25,32 @@ __device__ __forceinline__ void scale_units(const GradEntry &e, uint32_t ua, uin
     const char *in = static_cast<const char *>(e.in);
     char *out = static_cast<char *>(e.out);
     const int shift = behind<BI>(in - h * BI);    // of the input's groups against the output's
-    constexpr int per = kOptThreads * 2 / BI;     // groups per unit
-    const int64_t end = min((int64_t)ub * per, (numel + h + 7) / 8);
+    constexpr int per = kUnitVecs * 2 / BI;       // groups per unit
+    const int64_t end = min(((int64_t)unit + 1) * per, (numel + h + 7) / 8);
     // groups that can be taken whole: [lo, hi)
     const int64_t lo = (h + shift + 7) / 8, hi = (numel + h - (shift ? 8 - shift : 0)) / 8;
-    for (int64_t q = (int64_t)ua * per + threadIdx.x; q < end; q += kDepth * kOptThreads) {
-        if (q >= lo && q + (kDepth - 1) * kOptThreads < min(hi, end)) {
-            Raw<BI> r[kDepth];
+    constexpr int depth = kDepthBytes / (8 * BI);
+    const int lane = threadIdx.x % 32;
+    for (int64_t row = (int64_t)unit * per; row < end; row += depth * 32) {
+        const int64_t q = row + lane;
+        if (row >= lo && row + depth * 32 <= min(hi, end)) {
+            Raw<BI> r[depth];
+            const char *p = in + (row * 8 - h - shift) * BI;
+            if (shift)
+                load_shifted_rows(r, p, shift);
+            else
 #pragma unroll
-            for (int d = 0; d < kDepth; ++d) {
-                const char *p = in + ((q + d * kOptThreads) * 8 - h - shift) * BI;
-                r[d] = shift ? load_shifted<BI>(p, shift) : load_raw(p, (Raw<BI> *)nullptr);
-            }
+                for (int d = 0; d < depth; ++d) r[d] = load_raw(p + (d * 32 + lane) * 8 * BI, (Raw<BI> *)nullptr);
 #pragma unroll
-            for (int d = 0; d < kDepth; ++d) {
+            for (int d = 0; d < depth; ++d) {
                 float f[8];
                 to_floats(r[d], bi, f);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) f[j] *= c;
-                store_floats<BO>(out + ((q + d * kOptThreads) * 8 - h) * BO, f, bo);
+                store_floats<BO>(out + ((q + d * 32) * 8 - h) * BO, f, bo);
             }
         } else {
-            for (int64_t p = q; p < min(end, q + kDepth * kOptThreads); p += kOptThreads) {
+            for (int64_t p = q; p < min(end, row + depth * 32); p += 32) {
                 const int64_t i = p * 8 - h;      // the group's first element
                 if (p >= lo && p < hi) {
                     float f[8];
@@ -65,69 +68,58 @@ __device__ __forceinline__ void scale_units(const GradEntry &e, uint32_t ua, uin
     }
 }
 
-__device__ __forceinline__ void scale_units(const GradEntry &e, uint32_t ua, uint32_t ub, float c)
+__device__ __forceinline__ void scale_unit(const GradEntry &e, uint32_t unit, float c)
 {
     if (c == 1.0f && e.in == e.out) return;
     if (e.type() == ASPIS_F32) {
         if (e.out_type() == ASPIS_F32)
-            scale_units<4, 4>(e, ua, ub, c);
+            scale_unit<4, 4>(e, unit, c);
         else
-            scale_units<4, 2>(e, ua, ub, c);
+            scale_unit<4, 2>(e, unit, c);
     } else {
         if (e.out_type() == ASPIS_F32)
-            scale_units<2, 4>(e, ua, ub, c);
+            scale_unit<2, 4>(e, unit, c);
         else
-            scale_units<2, 2>(e, ua, ub, c);
+            scale_unit<2, 2>(e, unit, c);
     }
 }
 
 template <int N>
-__global__ void __launch_bounds__(kOptThreads, 6)
+__global__ void __launch_bounds__(kOptThreads, 4)
 scale_kernel(const __grid_constant__ Table<GradEntry, N> t, float max_norm, float scale, const float *norm, bool chained)
 {
     if (chained) chain();
     const float c = scale * clip_coef(*norm, max_norm);
     if (c == 1.0f && t.in_place) return;
-    const uint32_t runs = (t.units + kRun - 1) / kRun;
-    for (uint32_t r = blockIdx.x; r < runs; r += gridDim.x) {
-        uint32_t u = (runs - 1 - r) * kRun;
-        const uint32_t end = min(u + kRun, t.units);
-        for (int k = entry_of(t, u); u < end; ++k) {
-            const GradEntry &e = t.e[k];
-            const uint32_t stop = min(end, e.end);
-            scale_units(e, u - e.begin, stop - e.begin, c);
-            u = stop;
-        }
+    for (uint32_t r = blockIdx.x * kWarps + threadIdx.x / 32; r < t.units; r += gridDim.x * kWarps) {
+        const uint32_t u = t.units - 1 - r;
+        const GradEntry &e = t.e[entry_of(t, u)];
+        scale_unit(e, u - e.begin, c);
     }
 }
 
 // Norm and clipping in one cooperative kernel: every block sums a run of units, waits for the others, and
-// scales the same run.
+// scales the same run, which L1 or L2 still holds.
 template <int N>
 __global__ void __launch_bounds__(kOptThreads, kTogether)
 clip_kernel(const __grid_constant__ Table<GradEntry, N> t, float max_norm, float scale, float *norm, NormWork *work)
 {
-    const uint32_t begin = run_begin(t.units, blockIdx.x, gridDim.x), end = run_begin(t.units, blockIdx.x + 1, gridDim.x);
-    const int first = entry_of(t, begin);
+    const uint32_t begin = run_begin(t.units, blockIdx.x, gridDim.x) + threadIdx.x / 32;
+    const uint32_t end = run_begin(t.units, blockIdx.x + 1, gridDim.x);
     Sum sum;
-    uint32_t u = begin;
-    for (int k = first; u < end; ++k) {
-        const GradEntry &e = t.e[k];
-        const uint32_t stop = min(end, e.end);
-        sum_units(sum, e.in, e.numel(), e.type(), u - e.begin, stop - e.begin);
-        u = stop;
+    for (uint32_t u = begin; u < end; u += kWarps) {
+        const GradEntry &e = t.e[entry_of(t, u)];
+        const int64_t a = (int64_t)(u - e.begin) * kUnitVecs;
+        sum_range<32>(sum, e.in, e.numel(), e.type(), a, a + kUnitVecs, threadIdx.x % 32);
     }
     float all;
     const bool met = meet(sum, scale, work, all);
     if (blockIdx.x == 0 && threadIdx.x == 0) *norm = all;
     if (!met) return;
     const float c = scale * clip_coef(all, max_norm);
-    u = begin;
-    for (int k = first; u < end; ++k) {
-        const GradEntry &e = t.e[k];
-        const uint32_t stop = min(end, e.end);
-        scale_units(e, u - e.begin, stop - e.begin, c);
-        u = stop;
+    for (uint32_t u = begin; u < end; u += kWarps) {
+        const GradEntry &e = t.e[entry_of(t, u)];
+        scale_unit(e, u - e.begin, c);
     }
 }
 
@@ -135,9 +127,9 @@ template <int N>
 cudaError_t launch(const GradTable &t, float max_norm, float scale, const float *norm, bool chained,
                    cudaStream_t stream)
 {
-    const int64_t runs = ((int64_t)t.units + kRun - 1) / kRun;
-    const int64_t most = t.in_place ? (int64_t)sm_count() * kBlocks : runs;
-    const int64_t grid = runs < most ? runs : most;
+    const int64_t all = ((int64_t)t.units + kWarps - 1) / kWarps;
+    const int64_t most = t.in_place ? (int64_t)sm_count() * kBlocks : all;
+    const int64_t grid = all < most ? all : most;
     if (grid == 0) return cudaSuccess;
     void *args[] = {(void *)&t, &max_norm, &scale, &norm, &chained};
     return launch_table((const void *)scale_kernel<N>, grid, args, chained, stream);
@@ -147,9 +139,9 @@ template <int N>
 bool launch_clip(cudaError_t &err, const GradTable &t, float max_norm, float scale, float *norm, void *work,
                  cudaStream_t stream)
 {
-    const int64_t most = (int64_t)sm_count() * kTogether;
+    const int64_t all = ((int64_t)t.units + kWarps - 1) / kWarps, most = (int64_t)sm_count() * kTogether;
     void *args[] = {(void *)&t, &max_norm, &scale, &norm, &work};
-    return launch_together(err, (const void *)clip_kernel<N>, t.units < most ? t.units : most, args, stream);
+    return launch_together(err, (const void *)clip_kernel<N>, all < most ? all : most, args, stream);
 }
 
 }  // namespace

@@ -1,12 +1,12 @@
 // aspis_grad_norm: the global norm of many tensors.
 //
-// One kernel reads every element once.  A block takes a contiguous run of units,
-// adds the squares of each tensor that it meets and leaves one partial sum per
-// block, or, where the tensors' own norms are wanted, per (block, tensor).  The
-// pairs that occur form a staircase (a later block starts no earlier than at the
-// earlier one's last tensor), so block + tensor numbers them without collision.  The
-// last block to finish adds the partial sums in their order: the result depends on
-// the lengths and the grid alone, not on which block finished first.
+// One kernel reads every element once, and its last block to finish adds up the partial sums in
+// their order: the result depends on the lengths and the grid alone, not on which block
+// finished first.  Units are dealt to warps in turn, and a block leaves one partial sum.  Where the
+// tensors' own norms are wanted, a block takes a contiguous run of units and leaves one per
+// tensor that it meets.  The (block, tensor) pairs that occur then form a staircase (a later block starts
+// no earlier than at the earlier one's last tensor), so block + tensor numbers them without
+// collision.
 #include "norm.cuh"
 
 namespace aspis {
@@ -28,7 +28,7 @@ __device__ __forceinline__ void fetch(void *to, const void *from, uint32_t bytes
 template <int N>
 __global__ void __launch_bounds__(kOptThreads)
 norm_kernel(const __grid_constant__ Table<GradEntry, N> t, float scale, float *norm, float *tensor_norms,
-            NormWork *work, bool chained, uint32_t stretch)
+            NormWork *work, bool chained)
 {
     __shared__ BlockSums sh;
     __shared__ __align__(16) float2 parts[kMaxGrid + N];
@@ -47,27 +47,31 @@ norm_kernel(const __grid_constant__ Table<GradEntry, N> t, float scale, float *n
         }
         sum = Sum();
     };
-    // stretch 0: one run of units for each block, else runs of so many units dealt in turn
-    uint32_t u = stretch ? b * stretch : run_begin(t.units, b, grid);
-    while (u < t.units) {
-        const uint32_t end = stretch ? min(u + stretch, t.units) : run_begin(t.units, b + 1, grid);
-        for (int k = entry_of(t, u); u < end; ++k) {
+    if (!tensor_norms) {
+        // units dealt to the grid's warps in turn
+        for (uint32_t u = b * kWarps + threadIdx.x / 32; u < t.units; u += grid * kWarps) {
+            const GradEntry &e = t.e[entry_of(t, u)];
+            const int64_t a = (int64_t)(u - e.begin) * kUnitVecs;
+            sum_range<32>(sum, e.in, e.numel(), e.type(), a, a + kUnitVecs, threadIdx.x % 32);
+        }
+        leave(b);
+    } else {
+        // one run of units for each block, which leaves a partial sum for each tensor in it
+        uint32_t u = run_begin(t.units, b, grid);
+        const uint32_t end = run_begin(t.units, b + 1, grid);
+        for (int k = u < end ? entry_of(t, u) : 0; u < end; ++k) {
             const GradEntry &e = t.e[k];
-            const uint32_t stop = min(end, e.end), ua = u - e.begin, ub = stop - e.begin;
-            sum_units(sum, e.in, e.numel(), e.type(), ua, ub);
-            if (tensor_norms) {
-                leave(b + k);
-                if (threadIdx.x == 0) {
-                    if (u == e.begin) work->first[k] = (uint16_t)b;
-                    if (stop == e.end) work->last[k] = (uint16_t)b;
-                }
+            const uint32_t stop = min(end, e.end);
+            sum_range<kOptThreads>(sum, e.in, e.numel(), e.type(), (int64_t)(u - e.begin) * kUnitVecs,
+                                   (int64_t)(stop - e.begin) * kUnitVecs, threadIdx.x);
+            leave(b + k);
+            if (threadIdx.x == 0) {
+                if (u == e.begin) work->first[k] = (uint16_t)b;
+                if (stop == e.end) work->last[k] = (uint16_t)b;
             }
             u = stop;
         }
-        if (!stretch) break;
-        u += (grid - 1) * stretch;
     }
-    if (!tensor_norms) leave(b);
     // the last block adds up
     if (threadIdx.x == 0) {
         __threadfence();
@@ -124,12 +128,12 @@ template <int N>
 cudaError_t launch(const GradTable &t, float scale, float *norm, float *tensor_norms, void *work,
                    cudaStream_t stream)
 {
-    int64_t grid = (int64_t)sm_count() * 4;
+    const int64_t all = tensor_norms ? t.units : ((int64_t)t.units + kWarps - 1) / kWarps;
+    int64_t grid = (int64_t)sm_count() * 3;
     if (grid > kMaxGrid) grid = kMaxGrid;
-    if (grid > t.units) grid = t.units ? t.units : 1;
+    if (grid > all) grid = all ? all : 1;
     bool chained = t.first > 0;
-    uint32_t stretch = !tensor_norms && t.units >= 64 * (uint64_t)grid ? kVecs : 0;
-    void *args[] = {(void *)&t, &scale, &norm, &tensor_norms, &work, &chained, &stretch};
+    void *args[] = {(void *)&t, &scale, &norm, &tensor_norms, &work, &chained};
     return launch_table((const void *)norm_kernel<N>, grid, args, chained, stream);
 }
 

@@ -17,7 +17,6 @@
 
 namespace aspis {
 
-constexpr int kWarps = kOptThreads / 32;
 constexpr int kVecs = 8;                          // 16-byte vectors in flight per thread
 constexpr int kMostPolls = 1 << 22;               // of a wait for the other blocks
 constexpr uint32_t kWide = 1u << 16;              // in the count of blocks that are done: one had an fp64 sum
@@ -135,20 +134,19 @@ __device__ __forceinline__ double exact_squares(const uint4 &v)
     return s;
 }
 
-// One thread's share of the vectors [a, b) of a tensor (base: 16-byte aligned).  Plain loads: a
-// cooperative kernel may write what it has summed.
-template <int TYPE>
-__device__ __forceinline__ void sum_vectors(Sum &sum, const uint4 *base, int64_t a, int64_t b)
+// One thread's share (rank of TEAM) of the vectors [a, b) of a tensor (base: 16-byte aligned).  Plain
+// loads: a cooperative kernel may write what it has summed.
+template <int TYPE, int TEAM>
+__device__ __forceinline__ void sum_vectors(Sum &sum, const uint4 *base, int64_t a, int64_t b, int rank)
 {
-    for (int64_t v = a + threadIdx.x; v < b; v += kVecs * kOptThreads) {
+    for (int64_t v = a + rank; v < b; v += kVecs * TEAM) {
         uint4 r[kVecs];
-        if (v + (kVecs - 1) * kOptThreads < b) {
+        if (v + (kVecs - 1) * TEAM < b) {
 #pragma unroll
-            for (int u = 0; u < kVecs; ++u) r[u] = base[v + u * kOptThreads];
+            for (int u = 0; u < kVecs; ++u) r[u] = base[v + u * TEAM];
         } else {
 #pragma unroll
-            for (int u = 0; u < kVecs; ++u)
-                r[u] = v + u * kOptThreads < b ? base[v + u * kOptThreads] : make_uint4(0, 0, 0, 0);
+            for (int u = 0; u < kVecs; ++u) r[u] = v + u * TEAM < b ? base[v + u * TEAM] : make_uint4(0, 0, 0, 0);
         }
         float q[4] = {};
 #pragma unroll
@@ -164,29 +162,38 @@ __device__ __forceinline__ void sum_vectors(Sum &sum, const uint4 *base, int64_t
         for (int u = 0; u < kVecs; ++u) any |= (r[u].x | r[u].y) | (r[u].z | r[u].w);
         if ((any & (TYPE == ASPIS_F32 ? 0x7FFFFFFFu : 0x7FFF7FFFu)) == 0) continue;
 #pragma unroll 1
-        for (int u = 0; u < kVecs && v + u * kOptThreads < b; ++u)
-            sum.wide += exact_squares<TYPE>(base[v + u * kOptThreads]);
+        for (int u = 0; u < kVecs && v + u * TEAM < b; ++u) sum.wide += exact_squares<TYPE>(base[v + u * TEAM]);
     }
 }
 
-// One thread's share of units [ua, ub) of a tensor.  Vectors are counted from the 16-byte
-// boundary at or before its first element; those that it fills only in part, at either end, are
-// read element by element.
-template <int TYPE>
-__device__ __forceinline__ void sum_units(Sum &sum, const void *p, int64_t numel, uint32_t ua, uint32_t ub)
+// One thread's share of the vectors [a, b) of a tensor, counted from the 16-byte boundary at or
+// before its first element; those that it fills only in part, at either end, are read element by
+// element.
+template <int TYPE, int TEAM>
+__device__ __forceinline__ void sum_range(Sum &sum, const void *p, int64_t numel, int64_t a, int64_t b, int rank)
 {
     constexpr int per = 16 / type_bytes(TYPE);
     const int h = (int)((uintptr_t)p % 16) / type_bytes(TYPE);
     const uint4 *base = reinterpret_cast<const uint4 *>((uintptr_t)p - h * type_bytes(TYPE));
     const int64_t full = (h + numel) / per;                  // vectors before this one end inside the tensor
-    const int64_t a = (int64_t)ua * kOptThreads, b = (int64_t)ub * kOptThreads;
-    sum_vectors<TYPE>(sum, base, max(a, (int64_t)(h > 0)), min(b, full));
+    sum_vectors<TYPE, TEAM>(sum, base, max(a, (int64_t)(h > 0)), min(b, full), rank);
     const int64_t head = h > 0 ? min((int64_t)(per - h), numel) : 0;
-    if (threadIdx.x < 8) {
-        const int64_t i = threadIdx.x, j = max(full * per - h, head) + threadIdx.x;
-        if (ua == 0 && i < head) add_square(sum, load_one<type_bytes(TYPE)>(p, i, TYPE == ASPIS_BF16));
+    if (rank < 8) {
+        const int64_t i = rank, j = max(full * per - h, head) + rank;
+        if (a == 0 && i < head) add_square(sum, load_one<type_bytes(TYPE)>(p, i, TYPE == ASPIS_BF16));
         if (a <= full && full < b && j < numel) add_square(sum, load_one<type_bytes(TYPE)>(p, j, TYPE == ASPIS_BF16));
     }
+}
+
+template <int TEAM>
+__device__ __forceinline__ void sum_range(Sum &sum, const void *p, int64_t numel, int type, int64_t a, int64_t b, int rank)
+{
+    if (type == ASPIS_F32)
+        sum_range<ASPIS_F32, TEAM>(sum, p, numel, a, b, rank);
+    else if (type == ASPIS_BF16)
+        sum_range<ASPIS_BF16, TEAM>(sum, p, numel, a, b, rank);
+    else
+        sum_range<ASPIS_F16, TEAM>(sum, p, numel, a, b, rank);
 }
 
 // The block's sum, in thread 0; true (in every thread) where something needed fp64.
@@ -226,17 +233,6 @@ __device__ __forceinline__ float root(const Sum &sum, bool wide, float scale)
 {
     if (wide) return (float)(sqrt(sum.p.value() + sum.wide) * scale);
     return sqrtf(sum.p.hi + sum.p.lo) * scale;
-}
-
-// One thread's share of units of kParamUnit elements, or of units of the gradient's own size.
-__device__ __forceinline__ void sum_units(Sum &sum, const void *p, int64_t numel, int type, uint32_t ua, uint32_t ub)
-{
-    if (type == ASPIS_F32)
-        sum_units<ASPIS_F32>(sum, p, numel, ua, ub);
-    else if (type == ASPIS_BF16)
-        sum_units<ASPIS_BF16>(sum, p, numel, ua, ub);
-    else
-        sum_units<ASPIS_F16>(sum, p, numel, ua, ub);
 }
 
 // The norm inside a cooperative kernel: every block brings its sum and leaves with the norm of all,

@@ -11,7 +11,7 @@ using namespace aspis;
 
 namespace {
 
-constexpr int64_t kMostElements = (int64_t)1 << 40;      // keeps units within 32 bits
+constexpr int64_t kMostElements = (int64_t)1 << 38;      // keeps units within 31 bits
 
 bool known(int type) { return type == ASPIS_F32 || type == ASPIS_BF16 || type == ASPIS_F16; }
 

@@ -81,6 +81,7 @@ def test_struct_sizes():
     ((AT + 1, 5, ap.F16), ap.E_ALIGN),
     ((AT, 5, ap.F32, AT + 63, ap.BF16), ap.E_ALIGN),
     ((AT, (1 << 40) + 1, ap.F32), ap.E_RANGE),
+    ((AT, (1 << 38) + 1, ap.BF16), ap.E_RANGE),
 ])
 def test_tensor_lists(row, code):
     st, h = make(row)
