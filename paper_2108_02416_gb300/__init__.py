@@ -31,6 +31,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(PKG, "libaspis.so")
@@ -127,6 +128,11 @@ class _Param(ctypes.Structure):
                 ("numel", ctypes.c_int64), ("param_type", ctypes.c_int32),
                 ("grad_type", ctypes.c_int32), ("weight_decay", ctypes.c_float),
                 ("reserved", ctypes.c_int32)]
+
+
+# the same two, as list constructors write them
+_TENSOR, _PARAM = struct.Struct("=QQqii"), struct.Struct("=QQQQQqiifi")
+assert _TENSOR.size == ctypes.sizeof(_Tensor) and _PARAM.size == ctypes.sizeof(_Param)
 
 
 class _AdamwArgs(ctypes.Structure):
@@ -420,13 +426,11 @@ class TolerantBuffers(RoundBuffers):
 
 def _types():
     import torch
-    return {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+    return {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}, torch.strided
 
 
 def _gapless(t):
     """True when the tensor's elements fill its range of memory, in any order of dimensions."""
-    if t.is_contiguous():
-        return True
     at = 1
     for stride, size in sorted((st, n) for st, n in zip(t.stride(), t.shape) if n > 1):
         if stride != at:
@@ -435,36 +439,43 @@ def _gapless(t):
     return True
 
 
-def _tensor(t, types, device, name):
-    """The tensor's type code, after the checks that every tensor of a list has to pass."""
-    import torch
-    if t.layout != torch.strided or not t.is_cuda:
-        raise ValueError(f"{name} must be dense CUDA tensors")
-    if t.device != device:
-        raise ValueError(f"{name} must be on one device: got {t.device} and {device}")
-    code = types.get(t.dtype)
-    if code is None:
-        raise ValueError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
-    if not _gapless(t):
-        raise ValueError(f"{name} must fill their memory without gaps")
-    return code
-
-
-def _alike(t, other, name):
-    """Elementwise partners: the same shape, and the same order in memory."""
-    if t.shape != other.shape:
-        raise ValueError(f"{name}: shapes {tuple(t.shape)} and {tuple(other.shape)} differ")
-    if t.stride() != other.stride() and not (t.is_contiguous() and other.is_contiguous()):
-        raise ValueError(f"{name}: orders in memory (strides) differ")
-
-
 class _List:
     """Owns a list handle, and keeps its tensors' memory."""
     _create = _destroy = None
 
-    def __init__(self, items, n, device, kept):
+    def _start(self, first):
+        self._codes, self._strided = _types()
+        self.device = None if first is None else first.device
+        self._index = -1 if first is None else first.get_device()
+        self._kept = []
+
+    def _take(self, t, name):
+        """Checks a tensor, keeps its memory and gives its type's code and whether it is contiguous."""
+        if t.layout is not self._strided or t.get_device() < 0:
+            raise ValueError(f"{name} must be dense CUDA tensors")
+        if t.get_device() != self._index:
+            raise ValueError(f"{name} must be on one device: got {t.device} and {self.device}")
+        code = self._codes.get(t.dtype)
+        if code is None:
+            raise ValueError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
+        plain = t.is_contiguous()
+        if not plain and not _gapless(t):
+            raise ValueError(f"{name} must fill their memory without gaps")
+        self._kept.append(t.untyped_storage())
+        return code, plain
+
+    def _pair(self, t, plain, other, name):
+        """Checks the tensor that goes with t element by element: the same shape, and the same order in memory."""
+        code, plain_other = self._take(other, name)
+        if t.shape != other.shape:
+            raise ValueError(f"{name}: shapes {tuple(t.shape)} and {tuple(other.shape)} differ")
+        if not (plain and plain_other) and t.stride() != other.stride():
+            raise ValueError(f"{name}: orders in memory (strides) differ")
+        return code
+
+    def _make(self, items, n):
+        self.n = n
         self._h = ctypes.c_void_p()
-        self.n, self.device, self._kept = n, device, kept
         _ok(getattr(lib, self._create)(items, n, ctypes.byref(self._h)), self._create)
 
     def __len__(self):
@@ -495,25 +506,23 @@ class TensorList(_List):
         outs = [None] * len(tensors) if out is None else list(out)
         if len(outs) != len(tensors):
             raise ValueError(f"{len(tensors)} tensors and {len(outs)} outputs")
-        types, device = _types(), tensors[0].device if tensors else None
-        items = (_Tensor * len(tensors))()
-        for item, t, o in zip(items, tensors, outs):
-            item.type = _tensor(t, types, device, "tensors")
-            item.data, item.numel = t.data_ptr(), t.numel()
-            if o is not None:
-                item.out_type = _tensor(o, types, device, "out")
-                _alike(t, o, "out")
-                item.out = o.data_ptr()
-        super().__init__(items, len(tensors), device,
-                         [t.detach() for t in tensors + [o for o in outs if o is not None]])
+        self._start(tensors[0] if tensors else None)
+        items, at = (_Tensor * len(tensors))(), 0
+        for t, o in zip(tensors, outs):
+            code, plain = self._take(t, "tensors")
+            out_code = 0 if o is None else self._pair(t, plain, o, "out")
+            _TENSOR.pack_into(items, at, t.data_ptr(), 0 if o is None else o.data_ptr(), t.numel(), code, out_code)
+            at += _TENSOR.size
+        self._make(items, len(tensors))
 
 
 class ParamList(_List):
     """Parameters with their gradients and moments for :func:`aspis_adamw`.
 
-    ``exp_avg``, ``exp_avg_sq`` and ``masters`` are float32; ``masters`` (all of the
-    16-bit parameters', or None) hold the weights that the step is made on.
-    ``weight_decay``: one value, or one per tensor."""
+    ``exp_avg``, ``exp_avg_sq`` and ``masters`` are float32; ``masters`` (of the 16-bit
+    parameters, with None in the place of others, or None for none) hold the weights that
+    the step is made on.  ``weight_decay``: one value, or one per tensor.  The list
+    holds the tensors' memory as it is now."""
     _create, _destroy = "aspis_params_create", "aspis_params_destroy"
 
     def __init__(self, params, grads, exp_avg, exp_avg_sq, masters=None, weight_decay=0.0):
@@ -525,23 +534,18 @@ class ParamList(_List):
                         ("masters", masters), ("weight_decay", decay)):
             if len(x) != n:
                 raise ValueError(f"{n} params and {len(x)} {name}")
-        types, device = _types(), params[0].device if n else None
-        items = (_Param * n)()
-        for item, p, g, m, v, w, k in zip(items, params, grads, exp_avg, exp_avg_sq, masters, decay):
-            item.param_type = _tensor(p, types, device, "params")
-            item.grad_type = _tensor(g, types, device, "grads")
-            for name, x in (("grads", g), ("exp_avg", m), ("exp_avg_sq", v), ("masters", w)):
-                if x is None:
-                    continue
-                if name != "grads" and _tensor(x, types, device, name) != F32:
-                    raise ValueError(f"{name} must be float32")
-                _alike(p, x, name)
-            item.param, item.grad, item.numel = p.data_ptr(), g.data_ptr(), p.numel()
-            item.exp_avg, item.exp_avg_sq = m.data_ptr(), v.data_ptr()
-            item.master = None if w is None else w.data_ptr()
-            item.weight_decay = k
-        super().__init__(items, n, device, [t.detach() for x in (params, grads, exp_avg, exp_avg_sq, masters)
-                                            for t in x if t is not None])
+        self._start(params[0] if n else None)
+        items, at = (_Param * n)(), 0
+        for p, g, m, v, w, k in zip(params, grads, exp_avg, exp_avg_sq, masters, decay):
+            code, plain = self._take(p, "params")
+            grad_code = self._pair(p, plain, g, "grads")
+            if (self._pair(p, plain, m, "exp_avg") != F32 or self._pair(p, plain, v, "exp_avg_sq") != F32 or
+                    (w is not None and self._pair(p, plain, w, "masters") != F32)):
+                raise ValueError("exp_avg, exp_avg_sq and masters must be float32")
+            _PARAM.pack_into(items, at, p.data_ptr(), 0 if w is None else w.data_ptr(), g.data_ptr(),
+                             m.data_ptr(), v.data_ptr(), p.numel(), code, grad_code, k, 0)
+            at += _PARAM.size
+        self._make(items, n)
 
 
 class NormBuffers:
@@ -569,7 +573,7 @@ def _list_stream(x, stream):
         # the handle alone: a Stream object around it takes 2 us, a third of a small call
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         if raw is not None:
-            return raw(x.device.index)
+            return raw(x._index)
         return torch.cuda.current_stream(x.device).cuda_stream
     return _stream(stream)
 
