@@ -29,6 +29,9 @@
  *   - work is ASPIS_NORM_WORKSPACE_BYTES of device memory, 16-byte aligned,
  *     zeroed once by the caller; every call leaves it ready for the next.  Calls
  *     that may overlap on the GPU need a workspace (and a norm) each.
+ *   - Small lists are taken by one cooperative kernel, whose blocks wait for one another.  The
+ *     wait is bounded: were it ever to run out (seconds), the norm is NaN, nothing else is
+ *     written, and the workspace has to be zeroed again.
  *   - No call allocates, copies from the host or waits; all can be captured in a
  *     graph (with the arguments of the captured call, aspis_adamw's step too).
  */
@@ -112,9 +115,9 @@ aspis_status aspis_params_create(const aspis_param *params, int64_t n, aspis_par
 void aspis_params_destroy(aspis_params *list);
 
 typedef struct {
-    double lr;                   /* finite */
+    double lr;                   /* finite in fp32 */
     double beta1, beta2;         /* in [0, 1) */
-    double eps;                  /* >= 0, finite */
+    double eps;                  /* >= 0, finite; used in fp32 */
     int64_t step;                /* this step's number, from 1: bias corrections 1 - beta^step */
     float max_norm;              /* >= 0: clip to it (INFINITY: only the norm is taken);
                                     negative: no norm, no clipping */

@@ -190,7 +190,7 @@ auto by_types(const aspis_params::Group &g, F f)
 extern "C" aspis_status aspis_adamw(const aspis_params *params, const aspis_adamw_args *a, float *norm, void *work,
                                     void *stream)
 {
-    if (!params || !a || !isfinite(a->lr) || !(a->beta1 >= 0 && a->beta1 < 1) || !(a->beta2 >= 0 && a->beta2 < 1) ||
+    if (!params || !a || !isfinite((float)a->lr) || !(a->beta1 >= 0 && a->beta1 < 1) || !(a->beta2 >= 0 && a->beta2 < 1) ||
         !(a->eps >= 0) || isinf(a->eps) || a->step < 1 || isnan(a->max_norm) || !(a->scale > 0) || isinf(a->scale) ||
         a->reserved != 0)
         return ASPIS_E_INVAL;

@@ -191,7 +191,9 @@ cudaError_t launch_table(const void *kernel, int64_t grid, void **args, bool cha
     cfg.stream = stream;
     cfg.attrs = at;
     cfg.numAttrs = chained ? 1 : 0;
-    return cudaLaunchKernelExC(&cfg, kernel, args);
+    const cudaError_t e = cudaLaunchKernelExC(&cfg, kernel, args);
+    if (e != cudaSuccess) cudaGetLastError();     // the status says it; nobody else's call shall
+    return e;
 }
 
 bool launch_together(cudaError_t &err, const void *kernel, int64_t grid, void **args, cudaStream_t stream)
@@ -206,9 +208,8 @@ bool launch_together(cudaError_t &err, const void *kernel, int64_t grid, void **
     cfg.attrs = at;
     cfg.numAttrs = 1;
     err = cudaLaunchKernelExC(&cfg, kernel, args);
-    if (err != cudaErrorCooperativeLaunchTooLarge) return true;
-    cudaGetLastError();
-    return false;
+    if (err != cudaSuccess) cudaGetLastError();
+    return err != cudaErrorCooperativeLaunchTooLarge;
 }
 
 cudaError_t launch_grad_norm(const std::vector<std::unique_ptr<GradTable>> &tables, float scale, float *norm,

@@ -614,3 +614,130 @@ def test_python_refusals():
     with pytest.raises(ap.AspisError):
         ap.aspis_adamw(ap.ParamList([x], [a], [b], [c]), 0, 0.1)
     assert bool((x == 1).all())
+
+
+# ---------------------------------------------------------------- both sides of the rules on sizes
+
+
+def random_lengths(rng, most, count):
+    return [rng.choice([0, 1, 2, 7, 8, 9, 255, 256, 257]) if rng.random() < 0.4 else int(math.exp(rng.uniform(0, math.log(most))))
+            for _ in range(count)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("seed", range(12))
+def test_random_lists(seed):
+    """lists of random numbers, lengths, types and addresses, through every call with one workspace"""
+    import random
+    rng = random.Random(seed)
+    gen, buf = generator(100 + seed), ap.NormBuffers(DEV)
+    count = rng.choice([1, 5, 40, 130, 520, 1010])
+    lengths = random_lengths(rng, rng.choice([300, 20_000, 400_000]), count)
+    types = [rng.choice(TYPES) for _ in lengths]
+    grads = [views([n], d, rng.randrange(9), gen, 10.0 ** rng.uniform(-4, 1))[1][0] for n, d in zip(lengths, types)]
+    each = torch.zeros(count, device=DEV)
+    ap.aspis_grad_norm(ap.TensorList(grads), buf.norm, buf.work, tensor_norms=each)
+    want_each, want = norms(grads)
+    assert abs(float(buf.norm) - want) <= NORM * want
+    assert all(abs(x - y) <= NORM * y for x, y in zip(each.tolist(), want_each))
+    outs = [views([n], rng.choice(TYPES), rng.randrange(9), gen)[1][0] for n in lengths]
+    bound = want / 3
+    ap.aspis_clip_grads(ap.TensorList(grads, outs), bound, buf.norm, buf.work)
+    check_clip(grads, outs, coef(want, bound))
+    parts = []
+    for n, g in zip(lengths, grads):
+        p, off = rng.choice(TYPES), rng.randrange(9)
+        s = make_state([n], p, F32, p != F32 and rng.random() < 0.5, (off, 0), seed=rng.randrange(1 << 20))
+        s["g"], s["decay"] = (None, [g]), [rng.choice([0.0, 0.1])]
+        if rng.random() < 0.2:                           # a moment at another address than the rest
+            s["v"] = views([n], F32, (off + 3) % 9, gen, 1.0)
+            s["v"][1][0].square_()
+        parts.append(s)
+    olds = [copy_of(s) for s in parts]
+    cat = lambda k: [s[k][1][0] if s[k] else None for s in parts]  # noqa: E731
+    lst = ap.ParamList(cat("p"), grads, cat("m"), cat("v"), masters=cat("w"), weight_decay=[s["decay"][0] for s in parts])
+    ap.aspis_adamw(lst, 11, max_norm=bound, norm=buf.norm, work=buf.work, **HYPER)
+    assert abs(float(buf.norm) - want) <= NORM * want
+    for s, old in zip(parts, olds):
+        check_adamw(s, old, coef(want, bound), 11, **HYPER)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,out", [(F32, None), (F32, F32), (BF16, F32), (F16, F16), (F32, BF16)])
+@pytest.mark.parametrize("offset", [0, 3])
+def test_clip_of_more_than_one_kernel_takes(dtype, out, offset):
+    """a list too long for the cooperative kernel (64 MB of gradients), short tensors between long ones"""
+    lengths = [9_000_001, 3, 0, 1000, 1, 17_000_000 if dtype == F32 else 40_000_000, 77, 5]
+    _, ts = views(lengths, dtype, offset, generator(30))
+    before = [t.clone() for t in ts]
+    outs = ts if out is None else views(lengths, out, 0, generator(31))[1]
+    want = norms(before)[1]
+    got = clip(ts, None if out is None else outs, 0.25 * want)
+    assert abs(got - want) <= NORM * want
+    check_clip(before, outs, coef(want, 0.25 * want))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [8, 256, 257, 2_048, 600_000, 655_000, 656_000, 3_000_000])
+@pytest.mark.parametrize("ptype,gtype,master", [MIXES[0], MIXES[3], MIXES[9]])
+def test_adamw_on_both_sides_of_the_cooperative_kernel(n, ptype, gtype, master):
+    s = make_state([n, 5], ptype, gtype, master, (0, 1))
+    old, buf = copy_of(s), ap.NormBuffers(DEV)
+    ap.aspis_adamw(param_list(s), 3, max_norm=0.5, norm=buf.norm, work=buf.work, **HYPER)
+    check_adamw(s, old, coef(norms(old["g"])[1], 0.5), 3, **HYPER)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [5, 3_000, 20_000_000])
+@pytest.mark.parametrize("level", [1e-36, 1e-25, 1e22, 1e30])
+def test_clip_and_adamw_outside_the_range_of_fp32_squares(n, level):
+    x = (torch.rand(n, device=DEV, generator=generator(32)) + 0.5) * level
+    want, out, buf = norms([x])[1], torch.empty_like(x), ap.NormBuffers(DEV)
+    assert abs(clip([x], [out], want / 8) - want) <= NORM * want
+    check_clip([x], [out], coef(want, want / 8))
+    if level > 1:
+        p, m, v = torch.zeros_like(x), torch.zeros_like(x), torch.zeros_like(x)
+        ap.aspis_adamw(ap.ParamList([p], [x], [m], [v]), 1, 0.1, max_norm=1.0, norm=buf.norm, work=buf.work)
+        close(m, 0.1 * x.double() / want, 0.1 * x.double() / want * (FACTOR + 4 * U) + TINY)
+
+
+@pytest.mark.gpu
+def test_two_streams_with_buffers_of_their_own():
+    gen = generator(33)
+    lists = [[torch.randn(n, device=DEV, generator=gen) for n in (200_000 + i, 33, 1_000_000)] for i in range(2)]
+    handles, bufs = [ap.TensorList(x) for x in lists], [ap.NormBuffers(DEV) for _ in lists]
+    streams = [torch.cuda.Stream() for _ in lists]
+    want = [norms(x)[1] for x in lists]
+    torch.cuda.synchronize()
+    for _ in range(50):                                  # below the bound: the gradients stay as they are
+        for h, b, st in zip(handles, bufs, streams):
+            ap.aspis_clip_grads(h, 1e9, b.norm, b.work, stream=st)
+            ap.aspis_grad_norm(h, b.norm, b.work, stream=st)
+    torch.cuda.synchronize()
+    assert all(abs(float(b.norm) - w) <= NORM * w for b, w in zip(bufs, want))
+
+
+@pytest.mark.gpu
+def test_an_empty_list():
+    buf = ap.NormBuffers(DEV)
+    buf.norm.fill_(7.0)
+    ap.aspis_clip_grads(ap.TensorList([]), 1.0, buf.norm, buf.work)
+    assert float(buf.norm) == 0.0
+    buf.norm.fill_(7.0)
+    ap.aspis_adamw(ap.ParamList([], [], [], []), 1, 0.1, max_norm=1.0, norm=buf.norm, work=buf.work)
+    assert float(buf.norm) == 0.0
+    ap.aspis_adamw(ap.ParamList([], [], [], []), 1, 0.1)
+
+
+@pytest.mark.gpu
+def test_training_example():
+    import importlib.util
+    import os
+    from conftest import ROOT
+    spec = importlib.util.spec_from_file_location("train_step", os.path.join(ROOT, "examples", "train_step.py"))
+    mod = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(mod)
+    history = mod.train(steps=40, quiet=True)
+    assert all(math.isfinite(h["loss"]) and math.isfinite(h["norm"]) for h in history)
+    assert history[-1]["loss"] < 0.5 * history[0]["loss"]
+    assert all(h["clique"] == 5 for h in history)        # both adversaries found every time
