@@ -221,7 +221,7 @@ extern "C" aspis_status aspis_adamw(const aspis_params *params, const aspis_adam
             }))
             return err == cudaSuccess ? ASPIS_OK : ASPIS_E_CUDA;
     }
-    err = normed && work ? launch_grad_norm(params->grads.tables, a->scale, norm, nullptr, work, st)
+    err = normed && work ? launch_grad_norm(params->grads.tables, a->scale, norm, nullptr, work, true, st)
                                      : cudaSuccess;
     bool chained = normed && work;
     for (auto g = params->groups.rbegin(); g != params->groups.rend(); ++g)

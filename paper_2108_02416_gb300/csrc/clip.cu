@@ -160,7 +160,7 @@ extern "C" aspis_status aspis_clip_grads(const aspis_tensors *grads, float max_n
                                : launch_clip<kGrads>(e, t, max_norm, scale, norm, work, st))
             return e == cudaSuccess ? ASPIS_OK : ASPIS_E_CUDA;
     }
-    e = work ? launch_grad_norm(grads->tables, scale, norm, nullptr, work, st) : cudaSuccess;
+    e = work ? launch_grad_norm(grads->tables, scale, norm, nullptr, work, !grads->tables.back()->in_place, st) : cudaSuccess;
     bool chained = work != nullptr;
     for (auto it = grads->tables.rbegin(); it != grads->tables.rend() && e == cudaSuccess; ++it) {
         const GradTable &t = **it;

@@ -13,12 +13,29 @@ namespace aspis {
 
 namespace {
 
+// Of gradients that the next kernel reads again, from the end backwards, L2 is told to keep the last
+// 60 MB and to let the others go first.  Clipping 234 million bf16 into fp32 287 us without, 280 with 48 to 80 MB;
+// AdamW of 234 million parameters 1,010 and 994.  Lists that fit L2 are better off without (56 us and 57).  The
+// second kernel reads what was kept with the priority to go first; what it leaves behind cost 4 to 6 us in the next reads
+// of 88 MB that fit L2 themselves.
+constexpr uint32_t kKept = 15000;                 // units
+
+__device__ __forceinline__ uint64_t l2_policy(bool some, bool keep)
+{
+    uint64_t normal, first, last;
+    asm("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(normal));
+    asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(first));
+    asm("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(last));
+    return !some ? normal : keep ? last : first;
+}
+
 // Units of a tensor in a block's run from which on all warps take it together: 301 tensors of up
 // to 3 million bf16 values 49 us with 2 to 5, 54 with 8, 62 where every tensor was taken by all.
 constexpr uint32_t kApart = 4;
 // Of the last block: a thread adds up a tensor that fewer blocks than kFew met, else kLanes threads.  With
 // 8 threads for each 12.3 us for 256 small tensors (now 10.3), with one for each 33 for a ResNet-18's 62 (now 16.7).
 constexpr int kLanes = 8, kFew = 6;
+constexpr int kBlocks = 3;                        // per multiprocessor, each with 32 KB of gradient in flight (4: as fast or slower)
 
 // bytes from L2 into shared memory, in steps of 16
 __device__ __forceinline__ void fetch(void *to, const void *from, uint32_t bytes)
@@ -31,9 +48,9 @@ __device__ __forceinline__ void fetch(void *to, const void *from, uint32_t bytes
 }
 
 template <int N>
-__global__ void __launch_bounds__(kOptThreads)
+__global__ void __launch_bounds__(kOptThreads, kBlocks)
 norm_kernel(const __grid_constant__ Table<GradEntry, N> t, float scale, float *norm, float *tensor_norms,
-            NormWork *work, bool chained)
+            NormWork *work, bool chained, uint32_t kept)
 {
     __shared__ BlockSums sh;
     __shared__ __align__(16) float2 parts[kMaxGrid + N];
@@ -60,7 +77,8 @@ norm_kernel(const __grid_constant__ Table<GradEntry, N> t, float scale, float *n
         for (uint32_t u = b * kWarps + threadIdx.x / 32; u < t.units; u += grid * kWarps) {
             const GradEntry &e = t.e[entry_of(t, u)];
             const int64_t a = (int64_t)(u - e.begin) * kUnitVecs;
-            sum_range<32>(sum, e.in, e.numel(), e.type(), a, a + kUnitVecs, threadIdx.x % 32);
+            sum_range<32>(sum, e.in, e.numel(), e.type(), a, a + kUnitVecs, threadIdx.x % 32,
+                          PolicyLoad{l2_policy(kept, u + kept >= t.units)});
         }
         leave(b);
     } else {
@@ -165,16 +183,17 @@ norm_kernel(const __grid_constant__ Table<GradEntry, N> t, float scale, float *n
 }
 
 template <int N>
-cudaError_t launch(const GradTable &t, float scale, float *norm, float *tensor_norms, void *work,
+cudaError_t launch(const GradTable &t, float scale, float *norm, float *tensor_norms, void *work, bool again,
                    cudaStream_t stream)
 {
     const int per = tensor_norms ? 2 : kWarps;    // units, where there are few
     const int64_t all = ((int64_t)t.units + per - 1) / per;
-    int64_t grid = (int64_t)sm_count() * 3;
+    int64_t grid = (int64_t)sm_count() * kBlocks;
     if (grid > kMaxGrid) grid = kMaxGrid;
     if (grid > all) grid = all ? all : 1;
     bool chained = t.first > 0;
-    void *args[] = {(void *)&t, &scale, &norm, &tensor_norms, &work, &chained};
+    uint32_t kept = again && t.last && t.units > kKept ? kKept : 0;
+    void *args[] = {(void *)&t, &scale, &norm, &tensor_norms, &work, &chained, &kept};
     return launch_table((const void *)norm_kernel<N>, grid, args, chained, stream);
 }
 
@@ -213,12 +232,12 @@ bool launch_together(cudaError_t &err, const void *kernel, int64_t grid, void **
 }
 
 cudaError_t launch_grad_norm(const std::vector<std::unique_ptr<GradTable>> &tables, float scale, float *norm,
-                             float *tensor_norms, void *work, cudaStream_t stream)
+                             float *tensor_norms, void *work, bool again, cudaStream_t stream)
 {
     for (const auto &t : tables) {
-        const cudaError_t e = t->n <= kGradsSmall ? launch<kGradsSmall>(*t, scale, norm, tensor_norms, work, stream)
-                              : t->n <= kGradsMid ? launch<kGradsMid>(*t, scale, norm, tensor_norms, work, stream)
-                                                  : launch<kGrads>(*t, scale, norm, tensor_norms, work, stream);
+        const cudaError_t e = t->n <= kGradsSmall ? launch<kGradsSmall>(*t, scale, norm, tensor_norms, work, again, stream)
+                              : t->n <= kGradsMid ? launch<kGradsMid>(*t, scale, norm, tensor_norms, work, again, stream)
+                                                  : launch<kGrads>(*t, scale, norm, tensor_norms, work, again, stream);
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;
@@ -233,7 +252,7 @@ extern "C" aspis_status aspis_grad_norm(const aspis_tensors *grads, float scale,
 {
     if (!grads || !norm || !work || !(scale > 0.0f) || isinf(scale)) return ASPIS_E_INVAL;
     if ((uintptr_t)work % 16 != 0 || (uintptr_t)norm % 4 != 0 || (uintptr_t)tensor_norms % 4 != 0) return ASPIS_E_ALIGN;
-    return launch_grad_norm(grads->tables, scale, norm, tensor_norms, work, (cudaStream_t)stream) == cudaSuccess
+    return launch_grad_norm(grads->tables, scale, norm, tensor_norms, work, false, (cudaStream_t)stream) == cudaSuccess
                ? ASPIS_OK
                : ASPIS_E_CUDA;
 }

@@ -134,19 +134,38 @@ __device__ __forceinline__ double exact_squares(const uint4 &v)
     return s;
 }
 
-// One thread's share (rank of TEAM) of the vectors [a, b) of a tensor (base: 16-byte aligned).  Plain
-// loads: a cooperative kernel may write what it has summed.
-template <int TYPE, int TEAM>
-__device__ __forceinline__ void sum_vectors(Sum &sum, const uint4 *base, int64_t a, int64_t b, int rank)
+// How gradients are read: plainly (a cooperative kernel may write what it has summed), or with L2's
+// policy for them.
+struct PlainLoad {
+    __device__ __forceinline__ uint4 operator()(const uint4 *p) const { return *p; }
+};
+
+struct PolicyLoad {
+    uint64_t policy;
+
+    __device__ __forceinline__ uint4 operator()(const uint4 *p) const
+    {
+        uint4 v;
+        asm("ld.global.L2::cache_hint.v4.u32 {%0,%1,%2,%3}, [%4], %5;"
+            : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+            : "l"(p), "l"(policy));
+        return v;
+    }
+};
+
+// One thread's share (rank of TEAM) of the vectors [a, b) of a tensor (base: 16-byte aligned).
+template <int TYPE, int TEAM, class L>
+__device__ __forceinline__ void sum_vectors(Sum &sum, const uint4 *base, int64_t a, int64_t b, int rank, L load)
 {
     for (int64_t v = a + rank; v < b; v += kVecs * TEAM) {
         uint4 r[kVecs];
         if (v + (kVecs - 1) * TEAM < b) {
 #pragma unroll
-            for (int u = 0; u < kVecs; ++u) r[u] = base[v + u * TEAM];
+            for (int u = 0; u < kVecs; ++u) r[u] = load(base + v + u * TEAM);
         } else {
 #pragma unroll
-            for (int u = 0; u < kVecs; ++u) r[u] = v + u * TEAM < b ? base[v + u * TEAM] : make_uint4(0, 0, 0, 0);
+            for (int u = 0; u < kVecs; ++u)
+                r[u] = v + u * TEAM < b ? load(base + v + u * TEAM) : make_uint4(0, 0, 0, 0);
         }
         float q[4] = {};
 #pragma unroll
@@ -169,14 +188,14 @@ __device__ __forceinline__ void sum_vectors(Sum &sum, const uint4 *base, int64_t
 // One thread's share of the vectors [a, b) of a tensor, counted from the 16-byte boundary at or
 // before its first element; those that it fills only in part, at either end, are read element by
 // element.
-template <int TYPE, int TEAM>
-__device__ __forceinline__ void sum_range(Sum &sum, const void *p, int64_t numel, int64_t a, int64_t b, int rank)
+template <int TYPE, int TEAM, class L>
+__device__ __forceinline__ void sum_range(Sum &sum, const void *p, int64_t numel, int64_t a, int64_t b, int rank, L load)
 {
     constexpr int per = 16 / type_bytes(TYPE);
     const int h = (int)((uintptr_t)p % 16) / type_bytes(TYPE);
     const uint4 *base = reinterpret_cast<const uint4 *>((uintptr_t)p - h * type_bytes(TYPE));
     const int64_t full = (h + numel) / per;                  // vectors before this one end inside the tensor
-    sum_vectors<TYPE, TEAM>(sum, base, max(a, (int64_t)(h > 0)), min(b, full), rank);
+    sum_vectors<TYPE, TEAM>(sum, base, max(a, (int64_t)(h > 0)), min(b, full), rank, load);
     const int64_t head = h > 0 ? min((int64_t)(per - h), numel) : 0;
     if (rank < 8) {
         const int64_t i = rank, j = max(full * per - h, head) + rank;
@@ -185,15 +204,16 @@ __device__ __forceinline__ void sum_range(Sum &sum, const void *p, int64_t numel
     }
 }
 
-template <int TEAM>
-__device__ __forceinline__ void sum_range(Sum &sum, const void *p, int64_t numel, int type, int64_t a, int64_t b, int rank)
+template <int TEAM, class L = PlainLoad>
+__device__ __forceinline__ void sum_range(Sum &sum, const void *p, int64_t numel, int type, int64_t a, int64_t b, int rank,
+                                          L load = L())
 {
     if (type == ASPIS_F32)
-        sum_range<ASPIS_F32, TEAM>(sum, p, numel, a, b, rank);
+        sum_range<ASPIS_F32, TEAM>(sum, p, numel, a, b, rank, load);
     else if (type == ASPIS_BF16)
-        sum_range<ASPIS_BF16, TEAM>(sum, p, numel, a, b, rank);
+        sum_range<ASPIS_BF16, TEAM>(sum, p, numel, a, b, rank, load);
     else
-        sum_range<ASPIS_F16, TEAM>(sum, p, numel, a, b, rank);
+        sum_range<ASPIS_F16, TEAM>(sum, p, numel, a, b, rank, load);
 }
 
 // The block's sum, in thread 0; true (in every thread) where something needed fp64.

@@ -299,9 +299,10 @@ cudaError_t launch_table(const void *kernel, int64_t grid, void **args, bool cha
 // The same as a cooperative kernel; false (and nothing enqueued) where its blocks do not fit the device at once.
 bool launch_together(cudaError_t &err, const void *kernel, int64_t grid, void **args, cudaStream_t stream);
 
-// The norm of the list's gradients; norm (and tensor_norms) written by the last block.
+// The norm of the list's gradients; norm (and tensor_norms) written by the last block.  again: the call reads them
+// all once more, from the end of the list backwards.
 cudaError_t launch_grad_norm(const std::vector<std::unique_ptr<GradTable>> &tables, float scale, float *norm,
-                             float *tensor_norms, void *work, cudaStream_t stream);
+                             float *tensor_norms, void *work, bool again, cudaStream_t stream);
 
 }  // namespace aspis
 
