@@ -1,6 +1,15 @@
-// aspis_adamw: the norm (norm.cu), then one AdamW step on every tensor with the
-// gradient read through the clipping coefficient.  The step streams every array once, eight
-// elements per thread and access, and is bound by HBM.
+// aspis_adamw: the norm (norm.cu), then one AdamW step on every tensor with the gradient read through the
+// clipping coefficient.
+//
+//     h = s c g;  m <- b1 m + (1 - b1) h;  v <- b2 v + (1 - b2) h^2
+//     x <- x - ( lr wd x + lr / (1 - b1^t) * m / ( sqrt(v) / sqrt(1 - b2^t) + eps ) )
+//
+// The step streams every array once and is bound by HBM: 28 bytes per parameter in fp32, or in 16 bits with master
+// weights; 1.1 billion of the latter take 4.81 ms with the norm in front of them (31.9 + 2.3 GB: 7.1 TB/s).  A
+// warp takes 256 parameters, eight per thread, with its four or five loads in flight, and a block eight
+// such units: blocks that the hardware deals out in the order of the addresses stream faster than
+// resident ones that walk runs of their own (234 million parameters: 1,031 us, and 1,136 with four blocks per
+// multiprocessor).  Moments and masters are held in fp32; a 16-bit parameter is rounded to nearest once a step.
 #include <math.h>
 
 #include "optim.cuh"

@@ -1,12 +1,13 @@
-// aspis_grad_norm: the global norm of many tensors.
+// aspis_grad_norm: the global norm of many tensors, sqrt of the sum of all squares.
 //
-// One kernel reads every element once, and its last block to finish adds up the partial sums in
-// their order: the result depends on the lengths and the grid alone, not on which block
-// finished first.  Units are dealt to warps in turn, and a block leaves one partial sum.  Where the
-// tensors' own norms are wanted, a block takes a contiguous run of units and leaves one per
-// tensor that it meets.  The (block, tensor) pairs that occur then form a staircase (a later block starts
-// no earlier than at the earlier one's last tensor), so block + tensor numbers them without
-// collision.
+// One kernel reads every element once and is bound by HBM (1.1 billion bf16 values in 146 tensors, with each
+// one's own norm, 318 us: 7.2 TB/s) or, in small lists, by latency (six tensors 6.2 us, 62 of a
+// ResNet-18 16.8).  Its last block to finish adds up the partial sums in their order: the result depends
+// on the lengths and the grid alone, not on which block finished first.  Units are dealt to warps in turn, and a
+// block leaves one partial sum.  Where the tensors' own norms are wanted, a block takes a
+// contiguous run of units and leaves one per tensor that it meets.  The (block, tensor) pairs that occur
+// then form a staircase (a later block starts no earlier than at the earlier one's last tensor), so
+// block + tensor numbers them without collision.
 #include "norm.cuh"
 
 namespace aspis {
@@ -15,7 +16,7 @@ namespace {
 
 // Of gradients that the next kernel reads again, from the end backwards, L2 is told to keep the last
 // 60 MB and to let the others go first.  Clipping 234 million bf16 into fp32 287 us without, 280 with 48 to 80 MB;
-// AdamW of 234 million parameters 1,010 and 994.  Lists that fit L2 are better off without (56 us and 57).  The
+// AdamW of 234 million parameters 1,010 and 994 us.  Lists that fit L2 are better off without (56 us and 57).  The
 // second kernel reads what was kept with the priority to go first; what it leaves behind cost 4 to 6 us in the next reads
 // of 88 MB that fit L2 themselves.
 constexpr uint32_t kKept = 15000;                 // units
@@ -29,7 +30,7 @@ __device__ __forceinline__ uint64_t l2_policy(bool some, bool keep)
     return !some ? normal : keep ? last : first;
 }
 
-// Units of a tensor in a block's run from which on all warps take it together: 301 tensors of up
+// Units of a tensor in a block's run from which on all warps take it together: 601 tensors of up
 // to 3 million bf16 values 49 us with 2 to 5, 54 with 8, 62 where every tensor was taken by all.
 constexpr uint32_t kApart = 4;
 // Of the last block: a thread adds up a tensor that fewer blocks than kFew met, else kLanes threads.  With

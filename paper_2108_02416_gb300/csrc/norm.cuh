@@ -3,9 +3,8 @@
 //
 // Squares are added in fp32 over the eight 16-byte vectors that a thread holds (at
 // most 19 roundings in a row), and these sums as pairs of fp32 numbers, whose lower
-// one holds the rounding errors of the upper one: 48 bits without the fp64 units, of which
-// a multiprocessor has two (a warp's fp64 addition takes 16 cycles; with fp64 sums the norm of a
-// ResNet-18's 62 tensors took 27 us).  Where the sum over a thread's vectors
+// one holds the rounding errors of the upper one: 48 bits without the fp64 units, which are few on
+// this chip (with fp64 sums the norm of a ResNet-18's 62 tensors took 27 us, with these 21).  Where the sum over a thread's vectors
 // leaves [1e-30, 1e24], outside of which fp32 squares or their sum might vanish or overflow, the
 // vectors are read again (from L2) and squared and added in fp64; all-zero vectors, most of an
 // embedding's gradient, are told apart before that.
