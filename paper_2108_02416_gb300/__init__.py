@@ -451,6 +451,8 @@ class _List:
 
     def _take(self, t, name):
         """Checks a tensor, keeps its memory and gives its type's code and whether it is contiguous."""
+        if t is None:
+            raise ValueError(f"{name}: None is no tensor (leave parameters without a gradient out)")
         if t.layout is not self._strided or t.get_device() < 0:
             raise ValueError(f"{name} must be dense CUDA tensors")
         if t.get_device() != self._index:
@@ -498,7 +500,9 @@ class TensorList(_List):
 
     ``out``: tensors of the same shapes for the clipped values (any of the three
     types), or None to clip in place.  The list holds the tensors' memory as it is
-    now: make another when a gradient moves to other memory."""
+    now: make another when a gradient moves to other memory.  Calls run on the current
+    stream of the tensors' device, or on ``stream``; what other streams still do with
+    the tensors has to be waited for by the caller, as with any kernel."""
     _create, _destroy = "aspis_tensors_create", "aspis_tensors_destroy"
 
     def __init__(self, tensors, out=None):
