@@ -29,9 +29,9 @@
  *   - work is ASPIS_NORM_WORKSPACE_BYTES of device memory, 16-byte aligned,
  *     zeroed once by the caller; every call leaves it ready for the next.  Calls
  *     that may overlap on the GPU need a workspace (and a norm) each.
- *   - Small lists are taken by one cooperative kernel, whose blocks wait for one another.  The
- *     wait is bounded: were it ever to run out (seconds), the norm is NaN, nothing else is
- *     written, and the workspace has to be zeroed again.
+ *   - Clipping takes small lists in one cooperative kernel, whose blocks wait for one another.  The
+ *     wait is bounded: were it ever to run out (after seconds), the norm and the gradients are
+ *     undefined, and the workspace has to be zeroed again.
  *   - No call allocates, copies from the host or waits; all can be captured in a
  *     graph (with the arguments of the captured call, aspis_adamw's step too).
  */

@@ -256,7 +256,7 @@ __device__ __forceinline__ float root(const Sum &sum, bool wide, float scale)
 
 // The norm inside a cooperative kernel: every block brings its sum and leaves with the norm of all,
 // which every block adds up by itself, in the same order.  The wait is bounded (seconds); false
-// where it ran out, and then the norm is NaN and the caller leaves everything as it was.
+// where it ran out, and then the norm is NaN and the block has nothing more to do.
 __device__ __forceinline__ bool meet(Sum &sum, float scale, NormWork *work, float &norm)
 {
     __shared__ BlockSums sh;
