@@ -6,9 +6,11 @@
 // million bf16 into fp32 take 280 us (468 + 468 + 936 MB: 6.7 TB/s).  Below the bound a list in place is only
 // read: 936 MB in 136 us (6.9 TB/s).
 //
-// Up to 64 MB of gradients one cooperative kernel does both, its second pass reads L1 or L2: 65 thousand
-// bf16 values 6.8 us (two kernels 8.2), 17 million 18.5 (18.6), a ResNet-18's 11 million fp32 23.8 (26.6); 8.4
-// million bf16 13.7 (12.4), and from 75 MB on no less (33 us) or more (301 ragged fp16 tensors, 164 MB: 94 and 78).
+// Up to 64 MB of gradients one cooperative kernel does both: a warp's first unit waits in registers for the
+// norm (12.3 us for 8.4 million bf16 values in 256 tensors, 14.3 read again), the others come from L1 or L2.  60
+// thousand bf16 values take 7.5 us (two kernels 8.2), 200 thousand 8.2 (10.3), a ResNet-18's 11 million fp32
+// 22.7 (26.6), 17 million bf16 18.7 (18.6); from 75 MB on the two kernels are as fast (33 us) or faster (301 ragged
+// fp16 tensors, 164 MB: 94 and 78).
 #include "norm.cuh"
 
 using namespace aspis;
@@ -108,16 +110,67 @@ scale_kernel(const __grid_constant__ Table<GradEntry, N> t, float max_norm, floa
     }
 }
 
+// A warp's unit whose vectors stay in registers from the sum to the store, where the output's elements
+// have the same size and lie at the same place within 16 bytes.
+template <int TYPE>
+__device__ __forceinline__ void sum_held(Sum &sum, const GradEntry &e, uint32_t unit, uint4 (&r)[kVecs])
+{
+    const int lane = threadIdx.x % 32;
+    const Vectors<TYPE> t(e.in, e.numel());
+    const int64_t a = (int64_t)unit * kUnitVecs, b = a + kUnitVecs;
+    sum_batch<TYPE, 32>(sum, t.base(), max(a, (int64_t)(t.h > 0)) + lane, min(b, t.full), PlainLoad(), r);
+    t.ends(a, b, lane, [&](int64_t i) { add_square(sum, load_one<t.size>(e.in, i, TYPE == ASPIS_BF16)); });
+}
+
+template <int TYPE>
+__device__ __forceinline__ void store_held(const GradEntry &e, uint32_t unit, const uint4 (&r)[kVecs], float c)
+{
+    constexpr int size = type_bytes(TYPE);
+    const int lane = threadIdx.x % 32;
+    const bool bi = TYPE == ASPIS_BF16, bo = e.out_type() == ASPIS_BF16;
+    const Vectors<TYPE> t(e.in, e.numel());
+    const int64_t a = (int64_t)unit * kUnitVecs, b = a + kUnitVecs, end = min(b, t.full);
+    uint4 *out = reinterpret_cast<uint4 *>((uintptr_t)e.out - t.h * size);
+    const int64_t v = max(a, (int64_t)(t.h > 0)) + lane;
+#pragma unroll
+    for (int u = 0; u < kVecs; ++u) {
+        if (v + u * 32 >= end) break;
+        uint32_t w[4] = {r[u].x, r[u].y, r[u].z, r[u].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (size == 4) {
+                w[i] = __float_as_uint(__uint_as_float(w[i]) * c);
+            } else {
+                const float2 f = unpack(w[i], bi);
+                w[i] = pack(f.x * c, f.y * c, bo);
+            }
+        }
+        __stcs(out + v + u * 32, make_uint4(w[0], w[1], w[2], w[3]));
+    }
+    t.ends(a, b, lane, [&](int64_t i) { store_one<size>(e.out, i, load_one<size>(e.in, i, bi) * c, bo); });
+}
+
 // Norm and clipping in one cooperative kernel: every block sums a run of units, waits for the others, and
-// scales the same run, which L1 or L2 still holds.
+// scales the same run: a warp's first unit from registers, the others from what L1 or L2 still holds.
 template <int N>
 __global__ void __launch_bounds__(kOptThreads, kTogether)
 clip_kernel(const __grid_constant__ Table<GradEntry, N> t, float max_norm, float scale, float *norm, NormWork *work)
 {
     const uint32_t begin = run_begin(t.units, blockIdx.x, gridDim.x) + threadIdx.x / 32;
     const uint32_t end = run_begin(t.units, blockIdx.x + 1, gridDim.x);
+    const int first = begin < end ? entry_of(t, begin) : 0;
     Sum sum;
-    for (uint32_t u = begin; u < end; u += kWarps) {
+    uint4 held[kVecs];
+    if (begin < end) {
+        const GradEntry &e = t.e[first];
+        if (e.type() == ASPIS_F32)
+            sum_held<ASPIS_F32>(sum, e, begin - e.begin, held);
+        else if (e.type() == ASPIS_BF16)
+            sum_held<ASPIS_BF16>(sum, e, begin - e.begin, held);
+        else
+            sum_held<ASPIS_F16>(sum, e, begin - e.begin, held);
+    }
+    for (uint32_t u = begin + kWarps; u < end; u += kWarps) {
         const GradEntry &e = t.e[entry_of(t, u)];
         const int64_t a = (int64_t)(u - e.begin) * kUnitVecs;
         sum_range<32>(sum, e.in, e.numel(), e.type(), a, a + kUnitVecs, threadIdx.x % 32);
@@ -127,7 +180,21 @@ clip_kernel(const __grid_constant__ Table<GradEntry, N> t, float max_norm, float
     if (blockIdx.x == 0 && threadIdx.x == 0) *norm = all;
     if (!met) return;
     const float c = scale * clip_coef(all, max_norm);
-    for (uint32_t u = begin; u < end; u += kWarps) {
+    if (begin < end) {
+        const GradEntry &e = t.e[first];
+        if (type_bytes(e.type()) == type_bytes(e.out_type()) && ((uintptr_t)e.in - (uintptr_t)e.out) % 16 == 0) {
+            if (c == 1.0f && e.in == e.out) {
+            } else if (e.type() == ASPIS_F32)
+                store_held<ASPIS_F32>(e, begin - e.begin, held, c);
+            else if (e.type() == ASPIS_BF16)
+                store_held<ASPIS_BF16>(e, begin - e.begin, held, c);
+            else
+                store_held<ASPIS_F16>(e, begin - e.begin, held, c);
+        } else {
+            scale_unit(e, begin - e.begin, c);
+        }
+    }
+    for (uint32_t u = begin + kWarps; u < end; u += kWarps) {
         const GradEntry &e = t.e[entry_of(t, u)];
         scale_unit(e, u - e.begin, c);
     }

@@ -152,55 +152,75 @@ struct PolicyLoad {
     }
 };
 
-// One thread's share (rank of TEAM) of the vectors [a, b) of a tensor (base: 16-byte aligned).
+// The squares of the eight vectors v, v + TEAM, ... (those before b) of a tensor (base: 16-byte aligned),
+// which stay in r (zeros beyond b).
 template <int TYPE, int TEAM, class L>
-__device__ __forceinline__ void sum_vectors(Sum &sum, const uint4 *base, int64_t a, int64_t b, int rank, L load)
+__device__ __forceinline__ void sum_batch(Sum &sum, const uint4 *base, int64_t v, int64_t b, L load, uint4 (&r)[kVecs])
 {
-    for (int64_t v = a + rank; v < b; v += kVecs * TEAM) {
-        uint4 r[kVecs];
-        if (v + (kVecs - 1) * TEAM < b) {
+    if (v + (kVecs - 1) * TEAM < b) {
 #pragma unroll
-            for (int u = 0; u < kVecs; ++u) r[u] = load(base + v + u * TEAM);
-        } else {
+        for (int u = 0; u < kVecs; ++u) r[u] = load(base + v + u * TEAM);
+    } else {
 #pragma unroll
-            for (int u = 0; u < kVecs; ++u)
-                r[u] = v + u * TEAM < b ? load(base + v + u * TEAM) : make_uint4(0, 0, 0, 0);
-        }
-        float q[4] = {};
-#pragma unroll
-        for (int u = 0; u < kVecs; ++u) add_squares<TYPE>(q, r[u]);
-        const float s = (q[0] + q[1]) + (q[2] + q[3]);
-        // fp16 squares lie between 3.6e-15 and 4.3e9
-        if (TYPE == ASPIS_F16 ? s <= 1e24f : in_range(s)) {
-            sum.p.add(s);
-            continue;
-        }
-        uint32_t any = 0;
-#pragma unroll
-        for (int u = 0; u < kVecs; ++u) any |= (r[u].x | r[u].y) | (r[u].z | r[u].w);
-        if ((any & (TYPE == ASPIS_F32 ? 0x7FFFFFFFu : 0x7FFF7FFFu)) == 0) continue;
-#pragma unroll 1
-        for (int u = 0; u < kVecs && v + u * TEAM < b; ++u) sum.wide += exact_squares<TYPE>(base[v + u * TEAM]);
+        for (int u = 0; u < kVecs; ++u) r[u] = v + u * TEAM < b ? load(base + v + u * TEAM) : make_uint4(0, 0, 0, 0);
     }
+    float q[4] = {};
+#pragma unroll
+    for (int u = 0; u < kVecs; ++u) add_squares<TYPE>(q, r[u]);
+    const float s = (q[0] + q[1]) + (q[2] + q[3]);
+    // fp16 squares lie between 3.6e-15 and 4.3e9
+    if (TYPE == ASPIS_F16 ? s <= 1e24f : in_range(s)) {
+        sum.p.add(s);
+        return;
+    }
+    uint32_t any = 0;
+#pragma unroll
+    for (int u = 0; u < kVecs; ++u) any |= (r[u].x | r[u].y) | (r[u].z | r[u].w);
+    if ((any & (TYPE == ASPIS_F32 ? 0x7FFFFFFFu : 0x7FFF7FFFu)) == 0) return;
+#pragma unroll 1
+    for (int u = 0; u < kVecs && v + u * TEAM < b; ++u) sum.wide += exact_squares<TYPE>(base[v + u * TEAM]);
 }
 
-// One thread's share of the vectors [a, b) of a tensor, counted from the 16-byte boundary at or
-// before its first element; those that it fills only in part, at either end, are read element by
-// element.
+// A tensor's vectors are counted from the 16-byte boundary at or before its first element.
+template <int TYPE>
+struct Vectors {
+    static constexpr int size = type_bytes(TYPE), per = 16 / size;
+    const void *p;
+    int64_t numel;
+    int h;                        // elements before the first one
+    int64_t full;                 // vectors before this one end inside the tensor
+
+    __device__ __forceinline__ Vectors(const void *q, int64_t n)
+        : p(q), numel(n), h((int)((uintptr_t)q % 16) / size), full((h + n) / per)
+    {
+    }
+    __device__ __forceinline__ const uint4 *base() const
+    {
+        return reinterpret_cast<const uint4 *>((uintptr_t)p - h * size);
+    }
+    // f of each element of [a, b) in a vector that the tensor fills only in part, at either end
+    template <class F>
+    __device__ __forceinline__ void ends(int64_t a, int64_t b, int rank, F f) const
+    {
+        if (rank >= 8) return;
+        const int64_t head = h > 0 ? min((int64_t)(per - h), numel) : 0;
+        const int64_t i = rank, j = max(full * per - h, head) + rank;
+        if (a == 0 && i < head) f(i);
+        if (a <= full && full < b && j < numel) f(j);
+    }
+};
+
+// One thread's share (rank of TEAM) of the vectors [a, b) of a tensor.
 template <int TYPE, int TEAM, class L>
 __device__ __forceinline__ void sum_range(Sum &sum, const void *p, int64_t numel, int64_t a, int64_t b, int rank, L load)
 {
-    constexpr int per = 16 / type_bytes(TYPE);
-    const int h = (int)((uintptr_t)p % 16) / type_bytes(TYPE);
-    const uint4 *base = reinterpret_cast<const uint4 *>((uintptr_t)p - h * type_bytes(TYPE));
-    const int64_t full = (h + numel) / per;                  // vectors before this one end inside the tensor
-    sum_vectors<TYPE, TEAM>(sum, base, max(a, (int64_t)(h > 0)), min(b, full), rank, load);
-    const int64_t head = h > 0 ? min((int64_t)(per - h), numel) : 0;
-    if (rank < 8) {
-        const int64_t i = rank, j = max(full * per - h, head) + rank;
-        if (a == 0 && i < head) add_square(sum, load_one<type_bytes(TYPE)>(p, i, TYPE == ASPIS_BF16));
-        if (a <= full && full < b && j < numel) add_square(sum, load_one<type_bytes(TYPE)>(p, j, TYPE == ASPIS_BF16));
+    const Vectors<TYPE> t(p, numel);
+    const int64_t end = min(b, t.full);
+    for (int64_t v = max(a, (int64_t)(t.h > 0)) + rank; v < end; v += kVecs * TEAM) {
+        uint4 r[kVecs];
+        sum_batch<TYPE, TEAM>(sum, t.base(), v, end, load, r);
     }
+    t.ends(a, b, rank, [&](int64_t i) { add_square(sum, load_one<t.size>(p, i, TYPE == ASPIS_BF16)); });
 }
 
 template <int TEAM, class L = PlainLoad>
