@@ -110,15 +110,33 @@ scale_kernel(const __grid_constant__ Table<GradEntry, N> t, float max_norm, floa
     }
 }
 
-// A warp's unit whose vectors stay in registers from the sum to the store, where the output's elements
-// have the same size and lie at the same place within 16 bytes.
+// How the cooperative kernel counts a tensor's units.  Where the output's elements have the input's size and
+// lie at the same place within 16 bytes, both from the boundary of the output's groups, as scale_unit does: a
+// unit that waits in registers then has the elements that scale_unit would take, and its neighbours may be
+// left to either.  (fp32 groups are 32 bytes: units counted from the 16-byte boundary instead would begin four
+// elements away from scale_unit's for every second such address.)  Else the sum counts from the input's vectors,
+// and scale_unit alone stores.
+__device__ __forceinline__ bool stays_held(const GradEntry &e)
+{
+    return type_bytes(e.type()) == type_bytes(e.out_type()) && ((uintptr_t)e.in - (uintptr_t)e.out) % 16 == 0;
+}
+
+struct GroupOrigin {              // 16-bit groups are one vector
+    template <int TYPE>
+    __device__ __forceinline__ static int of(const GradEntry &e)
+    {
+        return TYPE == ASPIS_F32 && stays_held(e) ? behind<4>(e.out) : VectorOrigin::of<TYPE>(e);
+    }
+};
+
+// A warp's unit whose vectors stay in registers from the sum to the store.
 template <int TYPE>
 __device__ __forceinline__ void sum_held(Sum &sum, const GradEntry &e, uint32_t unit, uint4 (&r)[kVecs])
 {
     const int lane = threadIdx.x % 32;
-    const Vectors<TYPE> t(e.in, e.numel());
+    const Vectors<TYPE> t(e.in, e.numel(), GroupOrigin::of<TYPE>(e));
     const int64_t a = (int64_t)unit * kUnitVecs, b = a + kUnitVecs;
-    sum_batch<TYPE, 32>(sum, t.base(), max(a, (int64_t)(t.h > 0)) + lane, min(b, t.full), PlainLoad(), r);
+    sum_batch<TYPE, 32>(sum, t.base(), max(a, (int64_t)t.first) + lane, min(b, t.full), PlainLoad(), r);
     t.ends(a, b, lane, [&](int64_t i) { add_square(sum, load_one<t.size>(e.in, i, TYPE == ASPIS_BF16)); });
 }
 
@@ -128,10 +146,10 @@ __device__ __forceinline__ void store_held(const GradEntry &e, uint32_t unit, co
     constexpr int size = type_bytes(TYPE);
     const int lane = threadIdx.x % 32;
     const bool bi = TYPE == ASPIS_BF16, bo = e.out_type() == ASPIS_BF16;
-    const Vectors<TYPE> t(e.in, e.numel());
+    const Vectors<TYPE> t(e.in, e.numel(), GroupOrigin::of<TYPE>(e));
     const int64_t a = (int64_t)unit * kUnitVecs, b = a + kUnitVecs, end = min(b, t.full);
     uint4 *out = reinterpret_cast<uint4 *>((uintptr_t)e.out - t.h * size);
-    const int64_t v = max(a, (int64_t)(t.h > 0)) + lane;
+    const int64_t v = max(a, (int64_t)t.first) + lane;
 #pragma unroll
     for (int u = 0; u < kVecs; ++u) {
         if (v + u * 32 >= end) break;
@@ -173,7 +191,7 @@ clip_kernel(const __grid_constant__ Table<GradEntry, N> t, float max_norm, float
     for (uint32_t u = begin + kWarps; u < end; u += kWarps) {
         const GradEntry &e = t.e[entry_of(t, u)];
         const int64_t a = (int64_t)(u - e.begin) * kUnitVecs;
-        sum_range<32>(sum, e.in, e.numel(), e.type(), a, a + kUnitVecs, threadIdx.x % 32);
+        sum_range<32, GroupOrigin>(sum, e, a, a + kUnitVecs, threadIdx.x % 32);
     }
     float all;
     const bool met = meet(sum, scale, work, all);
@@ -182,7 +200,7 @@ clip_kernel(const __grid_constant__ Table<GradEntry, N> t, float max_norm, float
     const float c = scale * clip_coef(all, max_norm);
     if (begin < end) {
         const GradEntry &e = t.e[first];
-        if (type_bytes(e.type()) == type_bytes(e.out_type()) && ((uintptr_t)e.in - (uintptr_t)e.out) % 16 == 0) {
+        if (stays_held(e)) {
             if (c == 1.0f && e.in == e.out) {
             } else if (e.type() == ASPIS_F32)
                 store_held<ASPIS_F32>(e, begin - e.begin, held, c);

@@ -78,8 +78,7 @@ norm_kernel(const __grid_constant__ Table<GradEntry, N> t, float scale, float *n
         for (uint32_t u = b * kWarps + threadIdx.x / 32; u < t.units; u += grid * kWarps) {
             const GradEntry &e = t.e[entry_of(t, u)];
             const int64_t a = (int64_t)(u - e.begin) * kUnitVecs;
-            sum_range<32>(sum, e.in, e.numel(), e.type(), a, a + kUnitVecs, threadIdx.x % 32,
-                          PolicyLoad{l2_policy(kept, u + kept >= t.units)});
+            sum_range<32>(sum, e, a, a + kUnitVecs, threadIdx.x % 32, PolicyLoad{l2_policy(kept, u + kept >= t.units)});
         }
         leave(b);
     } else {
@@ -93,11 +92,11 @@ norm_kernel(const __grid_constant__ Table<GradEntry, N> t, float scale, float *n
             const uint32_t stop = min(end, e.end);
             const int64_t a = (int64_t)(u - e.begin) * kUnitVecs, z = (int64_t)(stop - e.begin) * kUnitVecs;
             if (stop - u >= kApart) {
-                sum_range<kOptThreads>(sum, e.in, e.numel(), e.type(), a, z, threadIdx.x);
+                sum_range<kOptThreads>(sum, e, a, z, threadIdx.x);
                 leave(b + k);
             } else if (turn++ % kWarps == threadIdx.x / 32) {
                 Sum x;
-                sum_range<32>(x, e.in, e.numel(), e.type(), a, z, threadIdx.x % 32);
+                sum_range<32>(x, e, a, z, threadIdx.x % 32);
                 const bool w = __any_sync(0xFFFFFFFFu, !(x.wide == 0));
                 x.p = group_sum<32>(x.p);
                 if (w) x.wide = group_sum<32>(x.wide);

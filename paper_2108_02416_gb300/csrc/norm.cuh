@@ -181,17 +181,19 @@ __device__ __forceinline__ void sum_batch(Sum &sum, const uint4 *base, int64_t v
     for (int u = 0; u < kVecs && v + u * TEAM < b; ++u) sum.wide += exact_squares<TYPE>(base[v + u * TEAM]);
 }
 
-// A tensor's vectors are counted from the 16-byte boundary at or before its first element.
+// A tensor's vectors are counted from a 16-byte boundary h elements before its first one: the last such
+// boundary, or the 32-byte one (h up to 7), where clipping counts groups of eight fp32 values from that.
 template <int TYPE>
 struct Vectors {
     static constexpr int size = type_bytes(TYPE), per = 16 / size;
     const void *p;
     int64_t numel;
-    int h;                        // elements before the first one
+    int h;
+    int first;                    // the first vector that begins inside the tensor
     int64_t full;                 // vectors before this one end inside the tensor
 
-    __device__ __forceinline__ Vectors(const void *q, int64_t n)
-        : p(q), numel(n), h((int)((uintptr_t)q % 16) / size), full((h + n) / per)
+    __device__ __forceinline__ Vectors(const void *q, int64_t n, int before)
+        : p(q), numel(n), h(before), first((h + per - 1) / per), full((h + n) / per)
     {
     }
     __device__ __forceinline__ const uint4 *base() const
@@ -203,36 +205,43 @@ struct Vectors {
     __device__ __forceinline__ void ends(int64_t a, int64_t b, int rank, F f) const
     {
         if (rank >= 8) return;
-        const int64_t head = h > 0 ? min((int64_t)(per - h), numel) : 0;
+        const int64_t head = min((int64_t)(first * per - h), numel);
         const int64_t i = rank, j = max(full * per - h, head) + rank;
         if (a == 0 && i < head) f(i);
         if (a <= full && full < b && j < numel) f(j);
     }
 };
 
+// h: the boundary at or before the first element
+struct VectorOrigin {
+    template <int TYPE>
+    __device__ __forceinline__ static int of(const GradEntry &e)
+    {
+        return (int)((uintptr_t)e.in % 16) / type_bytes(TYPE);
+    }
+};
+
 // One thread's share (rank of TEAM) of the vectors [a, b) of a tensor.
 template <int TYPE, int TEAM, class L>
-__device__ __forceinline__ void sum_range(Sum &sum, const void *p, int64_t numel, int64_t a, int64_t b, int rank, L load)
+__device__ __forceinline__ void sum_range(Sum &sum, const Vectors<TYPE> &t, int64_t a, int64_t b, int rank, L load)
 {
-    const Vectors<TYPE> t(p, numel);
     const int64_t end = min(b, t.full);
-    for (int64_t v = max(a, (int64_t)(t.h > 0)) + rank; v < end; v += kVecs * TEAM) {
+    for (int64_t v = max(a, (int64_t)t.first) + rank; v < end; v += kVecs * TEAM) {
         uint4 r[kVecs];
         sum_batch<TYPE, TEAM>(sum, t.base(), v, end, load, r);
     }
-    t.ends(a, b, rank, [&](int64_t i) { add_square(sum, load_one<t.size>(p, i, TYPE == ASPIS_BF16)); });
+    t.ends(a, b, rank, [&](int64_t i) { add_square(sum, load_one<t.size>(t.p, i, TYPE == ASPIS_BF16)); });
 }
 
-template <int TEAM, class L = PlainLoad>
-__device__ __forceinline__ void sum_range(Sum &sum, const void *p, int64_t numel, int type, int64_t a, int64_t b, int rank,
-                                          L load = L())
+template <int TEAM, class O = VectorOrigin, class L = PlainLoad>
+__device__ __forceinline__ void sum_range(Sum &sum, const GradEntry &e, int64_t a, int64_t b, int rank, L load = L())
 {
-    if (type == ASPIS_F32)
-        sum_range<ASPIS_F32, TEAM>(sum, p, numel, a, b, rank, load);
-    else if (type == ASPIS_BF16)
-        sum_range<ASPIS_BF16, TEAM>(sum, p, numel, a, b, rank, load);
+    if (e.type() == ASPIS_F32)
+        sum_range<ASPIS_F32, TEAM>(sum, Vectors<ASPIS_F32>(e.in, e.numel(), O::template of<ASPIS_F32>(e)), a, b, rank, load);
+    else if (e.type() == ASPIS_BF16)
+        sum_range<ASPIS_BF16, TEAM>(sum, Vectors<ASPIS_BF16>(e.in, e.numel(), O::template of<ASPIS_BF16>(e)), a, b, rank, load);
     else
-        sum_range<ASPIS_F16, TEAM>(sum, p, numel, a, b, rank, load);
+        sum_range<ASPIS_F16, TEAM>(sum, Vectors<ASPIS_F16>(e.in, e.numel(), O::template of<ASPIS_F16>(e)), a, b, rank, load);
 }
 
 // The block's sum, in thread 0; true (in every thread) where something needed fp64.
