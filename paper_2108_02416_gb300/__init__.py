@@ -561,6 +561,13 @@ class NormBuffers:
         self.work = torch.zeros(NORM_WORKSPACE_BYTES, dtype=torch.uint8, device=device)
 
 
+def _handle(x, kind, name):
+    """The list's handle: the library cannot tell one kind of list from another."""
+    if not isinstance(x, kind):
+        raise ValueError(f"{name} must be a {kind.__name__}, got {type(x).__name__}")
+    return x._h
+
+
 def _norm_args(norm, work):
     import torch
     if work is not None and work.numel() < NORM_WORKSPACE_BYTES:
@@ -586,10 +593,11 @@ def aspis_grad_norm(grads: TensorList, norm, work, tensor_norms=None, scale: flo
     """norm <- scale * the global L2 norm of ``grads``; ``tensor_norms`` (float32 [n]):
     every tensor's own."""
     import torch
+    handle = _handle(grads, TensorList, "grads")
     if tensor_norms is not None and tensor_norms.numel() < grads.n:
         raise ValueError(f"tensor_norms must have {grads.n} elements")
     np_, wp = _norm_args(norm, work)
-    _ok(lib.aspis_grad_norm(grads._h, scale, np_,
+    _ok(lib.aspis_grad_norm(handle, scale, np_,
                             None if tensor_norms is None else _dev(tensor_norms, torch.float32, "tensor_norms"),
                             wp, _list_stream(grads, stream)), "aspis_grad_norm")
 
@@ -597,8 +605,9 @@ def aspis_grad_norm(grads: TensorList, norm, work, tensor_norms=None, scale: flo
 def aspis_clip_grads(grads: TensorList, max_norm: float, norm, work=None, scale: float = 1.0, stream=None):
     """Clips ``grads`` to ``max_norm`` (into the list's outputs, or in place) and writes
     their norm; without ``work`` the norm is given in ``norm``."""
+    handle = _handle(grads, TensorList, "grads")
     np_, wp = _norm_args(norm, work)
-    _ok(lib.aspis_clip_grads(grads._h, max_norm, scale, np_, wp, _list_stream(grads, stream)),
+    _ok(lib.aspis_clip_grads(handle, max_norm, scale, np_, wp, _list_stream(grads, stream)),
         "aspis_clip_grads")
 
 
@@ -608,9 +617,10 @@ def aspis_adamw(params: ParamList, step: int, lr: float, betas=(0.9, 0.999), eps
     """One AdamW step (``step`` counts from 1).  ``max_norm``: clip by the global norm,
     which is written to ``norm``, or given there where ``work`` is None; None: no
     clipping.  ``skip_nonfinite``: change nothing where the norm is not finite."""
+    handle = _handle(params, ParamList, "params")
     args = _AdamwArgs(lr, betas[0], betas[1], eps, step, -1.0 if max_norm is None else max_norm, scale,
                       skip_nonfinite, 0)
     if max_norm is not None and max_norm < 0:
         raise ValueError("max_norm must not be negative")
     np_, wp = _norm_args(norm, work)
-    _ok(lib.aspis_adamw(params._h, ctypes.byref(args), np_, wp, _list_stream(params, stream)), "aspis_adamw")
+    _ok(lib.aspis_adamw(handle, ctypes.byref(args), np_, wp, _list_stream(params, stream)), "aspis_adamw")
