@@ -444,7 +444,12 @@ class _List:
     _create = _destroy = None
 
     def _start(self, first):
+        import torch
+        self._torch = torch
         self._codes, self._strided = _types()
+        self._current = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+        self._stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+            (lambda index: torch.cuda.current_stream(index).cuda_stream)
         self.device = None if first is None else first.device
         self._index = -1 if first is None else first.get_device()
         self._kept = []
@@ -501,7 +506,8 @@ class TensorList(_List):
     ``out``: tensors of the same shapes for the clipped values (any of the three
     types), or None to clip in place.  The list holds the tensors' memory as it is
     now: make another when a gradient moves to other memory.  Calls run on the current
-    stream of the tensors' device, or on ``stream``; what other streams still do with
+    stream of the tensors' device, whichever device is current, or on ``stream``; norm,
+    workspace and stream belong to that device.  What other streams still do with
     the tensors has to be waited for by the caller, as with any kernel."""
     _create, _destroy = "aspis_tensors_create", "aspis_tensors_destroy"
 
@@ -561,54 +567,64 @@ class NormBuffers:
         self.work = torch.zeros(NORM_WORKSPACE_BYTES, dtype=torch.uint8, device=device)
 
 
-def _handle(x, kind, name):
-    """The list's handle: the library cannot tell one kind of list from another."""
+def _open(x, kind, name, norm):
+    """The list's handle (the library cannot tell one kind of list from another), torch, and the device of the
+    call: the list's, or of an empty one its buffers'; -1 where there is none."""
     if not isinstance(x, kind):
         raise ValueError(f"{name} must be a {kind.__name__}, got {type(x).__name__}")
-    return x._h
+    index = x._index
+    return x._h, x._torch, index if index >= 0 or norm is None else norm.get_device()
 
 
-def _norm_args(norm, work):
-    import torch
-    if work is not None and work.numel() < NORM_WORKSPACE_BYTES:
-        raise ValueError(f"work must have {NORM_WORKSPACE_BYTES} bytes")
-    if norm is not None and norm.numel() < 1:
-        raise ValueError("norm must have an element")
-    return (None if norm is None else _dev(norm, torch.float32, "norm"),
-            None if work is None else _dev(work, torch.uint8, "work"))
+def _buffer(t, dtype, least, index, name):
+    """The address of a call's buffer on the call's device, or None."""
+    if t is None:
+        return None
+    if t.get_device() != index or index < 0:
+        raise ValueError(f"{name} must be a CUDA tensor on the list's device, got {t.device}")
+    if t.dtype is not dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.numel() < least:
+        raise ValueError(f"{name} must have {least} elements")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
 
 
-def _list_stream(x, stream):
-    if stream is None and x.device is not None:
-        import torch
-        # the handle alone: a Stream object around it takes 2 us, a third of a small call
-        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-        if raw is not None:
-            return raw(x._index)
-        return torch.cuda.current_stream(x.device).cuda_stream
-    return _stream(stream)
+def _launch(name, x, index, stream, *args):
+    """Calls the library on ``stream`` or the device's current stream, with the device current, as it launches
+    on the current one.  (Handles and device numbers alone: a Stream object takes 2 us, a third of a small call.)"""
+    if stream is None:
+        raw = x._stream_of(index) if index >= 0 else _stream(None)
+    else:
+        own = getattr(getattr(stream, "device", None), "index", None)
+        if index >= 0 and own is not None and own != index:
+            raise ValueError(f"stream must be on the list's device {index}, got {own}")
+        raw = _stream(stream)
+    if index < 0 or index == x._current():
+        status = getattr(lib, name)(*args, raw)
+    else:
+        with x._torch.cuda.device(index):
+            status = getattr(lib, name)(*args, raw)
+    if status != OK:
+        raise AspisError(status, name)
 
 
 def aspis_grad_norm(grads: TensorList, norm, work, tensor_norms=None, scale: float = 1.0, stream=None):
     """norm <- scale * the global L2 norm of ``grads``; ``tensor_norms`` (float32 [n]):
     every tensor's own."""
-    import torch
-    handle = _handle(grads, TensorList, "grads")
-    if tensor_norms is not None and tensor_norms.numel() < grads.n:
-        raise ValueError(f"tensor_norms must have {grads.n} elements")
-    np_, wp = _norm_args(norm, work)
-    _ok(lib.aspis_grad_norm(handle, scale, np_,
-                            None if tensor_norms is None else _dev(tensor_norms, torch.float32, "tensor_norms"),
-                            wp, _list_stream(grads, stream)), "aspis_grad_norm")
+    handle, torch, index = _open(grads, TensorList, "grads", norm)
+    _launch("aspis_grad_norm", grads, index, stream, handle, scale, _buffer(norm, torch.float32, 1, index, "norm"),
+            _buffer(tensor_norms, torch.float32, grads.n, index, "tensor_norms"),
+            _buffer(work, torch.uint8, NORM_WORKSPACE_BYTES, index, "work"))
 
 
 def aspis_clip_grads(grads: TensorList, max_norm: float, norm, work=None, scale: float = 1.0, stream=None):
     """Clips ``grads`` to ``max_norm`` (into the list's outputs, or in place) and writes
     their norm; without ``work`` the norm is given in ``norm``."""
-    handle = _handle(grads, TensorList, "grads")
-    np_, wp = _norm_args(norm, work)
-    _ok(lib.aspis_clip_grads(handle, max_norm, scale, np_, wp, _list_stream(grads, stream)),
-        "aspis_clip_grads")
+    handle, torch, index = _open(grads, TensorList, "grads", norm)
+    _launch("aspis_clip_grads", grads, index, stream, handle, max_norm, scale,
+            _buffer(norm, torch.float32, 1, index, "norm"), _buffer(work, torch.uint8, NORM_WORKSPACE_BYTES, index, "work"))
 
 
 def aspis_adamw(params: ParamList, step: int, lr: float, betas=(0.9, 0.999), eps: float = 1e-8,
@@ -617,10 +633,10 @@ def aspis_adamw(params: ParamList, step: int, lr: float, betas=(0.9, 0.999), eps
     """One AdamW step (``step`` counts from 1).  ``max_norm``: clip by the global norm,
     which is written to ``norm``, or given there where ``work`` is None; None: no
     clipping.  ``skip_nonfinite``: change nothing where the norm is not finite."""
-    handle = _handle(params, ParamList, "params")
+    handle, torch, index = _open(params, ParamList, "params", norm)
     args = _AdamwArgs(lr, betas[0], betas[1], eps, step, -1.0 if max_norm is None else max_norm, scale,
                       skip_nonfinite, 0)
     if max_norm is not None and max_norm < 0:
         raise ValueError("max_norm must not be negative")
-    np_, wp = _norm_args(norm, work)
-    _ok(lib.aspis_adamw(handle, ctypes.byref(args), np_, wp, _list_stream(params, stream)), "aspis_adamw")
+    _launch("aspis_adamw", params, index, stream, handle, ctypes.byref(args),
+            _buffer(norm, torch.float32, 1, index, "norm"), _buffer(work, torch.uint8, NORM_WORKSPACE_BYTES, index, "work"))

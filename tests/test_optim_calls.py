@@ -26,6 +26,9 @@ class Buffer:
         return self.index
 
 
+LAUNCHES = ("aspis_grad_norm", "aspis_clip_grads", "aspis_adamw")
+
+
 class Library:
     """Notes the calls that launch; the others go to the real one."""
 
@@ -33,7 +36,7 @@ class Library:
         self.real, self.calls = real, []
 
     def __getattr__(self, name):
-        if name in ("aspis_grad_norm", "aspis_clip_grads", "aspis_adamw"):
+        if name in LAUNCHES:
             def call(*args):
                 self.calls.append(name)
                 return ap.OK
@@ -41,11 +44,16 @@ class Library:
         return getattr(self.real, name)
 
 
+def current(monkeypatch, device):
+    monkeypatch.setattr(torch.cuda, "current_device", device)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", device, raising=False)
+
+
 @pytest.fixture
 def library(monkeypatch):
     lib = Library(ap.lib)
     monkeypatch.setattr(ap, "lib", lib)
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    current(monkeypatch, lambda: 0)
     return lib
 
 
@@ -60,7 +68,7 @@ def test_lists_of_the_other_kind(library):
     ap.aspis_grad_norm(grads, norm, work, stream=0)
     ap.aspis_clip_grads(grads, 1.0, norm, work, stream=0)
     ap.aspis_adamw(params, 1, 1e-3, max_norm=1.0, norm=norm, work=work, stream=0)
-    assert library.calls == ["aspis_grad_norm", "aspis_clip_grads", "aspis_adamw"]
+    assert library.calls == list(LAUNCHES)
     for wrong in (params, [], None):
         with pytest.raises(ValueError):
             ap.aspis_grad_norm(wrong, norm, work, stream=0)
@@ -70,3 +78,95 @@ def test_lists_of_the_other_kind(library):
         with pytest.raises(ValueError):
             ap.aspis_adamw(wrong, 1, 1e-3, stream=0)
     assert len(library.calls) == 3
+
+
+class Devices:
+    """Two devices: which one is current, and which was at each call of the library."""
+
+    def __init__(self, monkeypatch, library):
+        self.current, self.at, self.streams = 0, [], []
+        devices = self
+
+        class Guard:
+            def __init__(self, index):
+                self.index = index
+
+            def __enter__(self):
+                self.before, devices.current = devices.current, self.index
+
+            def __exit__(self, *_):
+                devices.current = self.before
+
+        class Noting:
+            def __getattr__(self, name):
+                call = getattr(library, name)
+                if name not in LAUNCHES:
+                    return call
+
+                def noted(*args):
+                    devices.at.append(devices.current)
+                    devices.streams.append(getattr(args[-1], "value", args[-1]) or 0)
+                    return call(*args)
+                return noted
+
+        monkeypatch.setattr(ap, "lib", Noting())
+        monkeypatch.setattr(torch.cuda, "device", Guard)
+        current(monkeypatch, lambda: self.current)
+        monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda index: 100 + index, raising=False)
+
+
+class Stream:
+    def __init__(self, index):
+        self.cuda_stream, self.device = 200 + index, torch.device("cuda", index)
+
+
+@pytest.fixture
+def devices(monkeypatch, library):
+    return Devices(monkeypatch, library)
+
+
+def lists(index):
+    """lists whose tensors lie on a device (empty ones: nothing would be launched on any address)"""
+    out = ap.TensorList([]), ap.ParamList([], [], [], [])
+    for x in out:
+        x._index, x.device = index, torch.device("cuda", index)
+    return out
+
+
+def every_call(grads, params, norm, work, each=None, stream=None):
+    return [lambda: ap.aspis_grad_norm(grads, norm, work, tensor_norms=each, stream=stream),
+            lambda: ap.aspis_clip_grads(grads, 1.0, norm, work, stream=stream),
+            lambda: ap.aspis_adamw(params, 1, 1e-3, max_norm=1.0, norm=norm, work=work, stream=stream)]
+
+
+@pytest.mark.parametrize("current", [0, 1])
+@pytest.mark.parametrize("own", [0, 1])
+def test_calls_run_on_the_lists_device(devices, own, current):
+    devices.current = current
+    for call in every_call(*lists(own), *buffers(own)):
+        call()
+    for call in every_call(*lists(own), *buffers(own), stream=Stream(own)):
+        call()
+    ap.aspis_adamw(lists(own)[1], 1, 1e-3)                   # no buffers
+    assert devices.at == [own] * 7 and devices.current == current
+    assert devices.streams == [100 + own] * 3 + [200 + own] * 3 + [100 + own]
+
+
+def test_an_empty_list_runs_where_its_buffers_are(devices):
+    for call in every_call(ap.TensorList([]), ap.ParamList([], [], [], []), *buffers(1)):
+        call()
+    assert devices.at == [1] * 3 and devices.streams == [101] * 3
+
+
+def test_buffers_and_streams_of_another_device(devices):
+    (norm0, work0), (norm1, work1) = buffers(0), buffers(1)
+    for norm, work in ((norm0, work1), (norm1, work0), (norm0, work0)):
+        for call in every_call(*lists(1), norm, work):
+            with pytest.raises(ValueError):
+                call()
+    for call in every_call(*lists(1), norm1, work1, stream=Stream(0)):
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(ValueError):
+        ap.aspis_grad_norm(lists(1)[0], norm1, work1, tensor_norms=Buffer(device=0))
+    assert devices.at == []
