@@ -25,7 +25,8 @@
  *     while it is within fp32's range itself.
  *   - NaN and infinity follow IEEE-754 through the formulas: an infinite norm
  *     makes c = 0 (finite gradients become 0, infinite ones NaN), a NaN makes
- *     everything NaN.  aspis_adamw can leave everything as it was instead.
+ *     everything NaN.  aspis_adamw can leave everything as it was instead.  An
+ *     infinite max_norm clips nothing: c = 1, whatever the norm.
  *   - work is ASPIS_NORM_WORKSPACE_BYTES of device memory, 16-byte aligned,
  *     zeroed once by the caller; every call leaves it ready for the next.  Calls
  *     that may overlap on the GPU need a workspace (and a norm) each.

@@ -272,9 +272,11 @@ __device__ __forceinline__ int behind(const void *p)
     return (int)((uintptr_t)p % (8 * B)) / B;
 }
 
-// min(1, max_norm / (norm + eps)); NaN stays NaN
+// min(1, max_norm / (norm + eps)), where NaN stays NaN; 1 for an infinite bound, whatever the norm (the
+// quotient would be NaN where that is infinite too)
 __device__ __forceinline__ float clip_coef(float norm, float max_norm)
 {
+    if (isinf(max_norm)) return 1.0f;
     const float c = max_norm / (norm + ASPIS_CLIP_EPS);
     return c > 1.0f ? 1.0f : c;
 }
