@@ -118,7 +118,7 @@ void aspis_params_destroy(aspis_params *list);
 typedef struct {
     double lr;                   /* finite in fp32 */
     double beta1, beta2;         /* in [0, 1) */
-    double eps;                  /* >= 0, finite; used in fp32 */
+    double eps;                  /* >= 0, finite in fp32, which it is used in */
     int64_t step;                /* this step's number, from 1: bias corrections 1 - beta^step */
     float max_norm;              /* >= 0: clip to it (INFINITY: only the norm is taken);
                                     negative: no norm, no clipping */

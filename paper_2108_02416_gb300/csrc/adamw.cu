@@ -165,7 +165,7 @@ extern "C" aspis_status aspis_adamw(const aspis_params *params, const aspis_adam
                                     void *stream)
 {
     if (!params || !a || !isfinite((float)a->lr) || !(a->beta1 >= 0 && a->beta1 < 1) || !(a->beta2 >= 0 && a->beta2 < 1) ||
-        !(a->eps >= 0) || isinf(a->eps) || a->step < 1 || isnan(a->max_norm) || !(a->scale > 0) || isinf(a->scale) ||
+        !(a->eps >= 0) || isinf((float)a->eps) || a->step < 1 || isnan(a->max_norm) || !(a->scale > 0) || isinf(a->scale) ||
         a->reserved != 0)
         return ASPIS_E_INVAL;
     const bool normed = a->max_norm >= 0;

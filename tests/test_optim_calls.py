@@ -170,3 +170,10 @@ def test_buffers_and_streams_of_another_device(devices):
     with pytest.raises(ValueError):
         ap.aspis_grad_norm(lists(1)[0], norm1, work1, tensor_norms=Buffer(device=0))
     assert devices.at == []
+
+
+@pytest.mark.parametrize("eps,code", [(3.4e38, "OK"), (3.5e38, "E_INVAL"), (1e300, "E_INVAL"), (0.0, "OK")])
+def test_eps_ends_where_fp32_does(eps, code):
+    """it is used in fp32, where these would be infinite and stop every parameter (an empty list: nothing is launched)"""
+    params, args = ap.ParamList([], [], [], []), ap._AdamwArgs(1e-3, 0.9, 0.999, eps, 1, -1.0, 1.0, 0, 0)
+    assert ap.lib.aspis_adamw(params._h, ap.ctypes.byref(args), None, None, None) == getattr(ap, code)
