@@ -177,3 +177,44 @@ def test_eps_ends_where_fp32_does(eps, code):
     """it is used in fp32, where these would be infinite and stop every parameter (an empty list: nothing is launched)"""
     params, args = ap.ParamList([], [], [], []), ap._AdamwArgs(1e-3, 0.9, 0.999, eps, 1, -1.0, 1.0, 0, 0)
     assert ap.lib.aspis_adamw(params._h, ap.ctypes.byref(args), None, None, None) == getattr(ap, code)
+
+
+class OnDevice:
+    """A host tensor that says it lies on a device: lists look at tensors and read none."""
+
+    def __init__(self, t):
+        self.t, self.device = t, torch.device("cuda", 0)
+
+    def __getattr__(self, name):
+        return getattr(self.t, name)
+
+    def get_device(self):
+        return 0
+
+
+def strided(shape, strides):
+    return OnDevice(torch.zeros(4096).as_strided(shape, strides))
+
+
+@pytest.mark.parametrize("shape,one,other,same", [
+    ((1, 5, 4, 3), (60, 1, 15, 5), (7, 1, 15, 5), True),         # channels last; a dimension of one has any stride
+    ((4, 1, 3), (1, 12, 4), (1, 1, 4), True),
+    ((4, 1, 3, 1), (1, 99, 4, 5), (1, 4, 4, 12), True),
+    ((4, 5, 3), (1, 12, 4), (1, 12, 4), True),
+    ((4, 5, 3), (1, 12, 4), (5, 1, 20), False),
+    ((4, 1, 3), (1, 12, 4), (3, 3, 1), False),                   # one in the other order
+    ((4, 1, 3), (3, 3, 1), (1, 12, 4), False),
+    ((2, 2), (1, 2), (2, 1), False),
+    ((1, 1), (9, 7), (1, 1), True),
+])
+def test_orders_in_memory(shape, one, other, same):
+    """element i of one tensor goes with element i of the other, wherever a dimension of length one claims to step to"""
+    def make():
+        a, b = strided(shape, one), strided(shape, other)
+        ap.TensorList([a], [b])
+        ap.ParamList([a], [b], [strided(shape, other)], [strided(shape, one)])
+    if same:
+        make()
+    else:
+        with pytest.raises(ValueError):
+            make()
