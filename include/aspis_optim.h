@@ -19,10 +19,13 @@
  *   - A tensor is `numel` elements without gaps, of fp32, bf16 or fp16, at any
  *     address that is a multiple of the element's size.  numel 0 is allowed (data
  *     may then be NULL).  One list may mix types, lengths and alignments.
- *   - Sums, norms and moments are held in 32 bits or more.  Sums of squares are
- *     added in 64 bits, in an order that depends on the lengths alone, so a call
- *     gives the same bits each time; a norm neither overflows nor vanishes
- *     while it is within fp32's range itself.
+ *   - Sums, norms and moments are held in 32 bits or more.  Up to 64 squares are
+ *     added in fp32, and such sums as pairs of fp32 numbers (48 bits), or in fp64
+ *     where they leave [1e-30, 1e24]: a norm neither overflows nor vanishes while
+ *     it is within fp32's range itself.  The order depends on the call, the list
+ *     (lengths, types, addresses modulo 32) and the device, so the same call gives
+ *     the same bits each time.  Other calls on the same values (with and without
+ *     tensor_norms, norm and clipping, copies elsewhere) may differ in the last bits.
  *   - NaN and infinity follow IEEE-754 through the formulas: an infinite norm
  *     makes c = 0 (finite gradients become 0, infinite ones NaN), a NaN makes
  *     everything NaN.  aspis_adamw can leave everything as it was instead.  An

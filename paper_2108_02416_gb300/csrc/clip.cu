@@ -7,9 +7,9 @@
 // read: 936 MB in 136 us (6.9 TB/s).
 //
 // Up to 64 MB of gradients one cooperative kernel does both: a warp's first unit waits in registers for the
-// norm (12.3 us for 8.4 million bf16 values in 256 tensors, 14.3 read again), the others come from L1 or L2.  60
+// norm (12.4 us for 8.4 million bf16 values in 256 tensors, 14.3 read again), the others come from L1 or L2.  60
 // thousand bf16 values take 7.5 us (two kernels 8.2), 200 thousand 8.2 (10.3), a ResNet-18's 11 million fp32
-// 22.7 (26.6), 17 million bf16 18.7 (18.6); from 75 MB on the two kernels are as fast (33 us) or faster (301 ragged
+// 22.8 (26.6), 17 million bf16 18.7 (18.6); from 75 MB on the two kernels are as fast (33 us) or faster (301 ragged
 // fp16 tensors, 164 MB: 94 and 78).
 #include "norm.cuh"
 
@@ -20,8 +20,9 @@ namespace {
 // That a thread loads before it stores.  Of 234 million bf16 into fp32 285 us, with 64 bytes 287, with 32 291; of 301
 // ragged fp16 tensors at odd addresses 83, 86 and 86.
 constexpr int kDepthBytes = 128;
-// Blocks per multiprocessor where the call may turn out to write nothing (else a block per eight units): 234
-// million fp32 in place 279 us clipped and 139.6 below the bound, 294 and 138.9 with 8, 270 and 168 with all of them.
+// Blocks per multiprocessor where the call may turn out to write nothing (else a block per eight units).  The whole
+// call on 234 million fp32 in place takes 401 us clipped (2.8 GB: 7.0 TB/s; scaling alone, with a given norm, 274) and
+// 139 below the bound; with 8 blocks 416 and 137, with a block per eight units 390 and 166.
 constexpr int kBlocks = 16;
 constexpr int kTogether = 3;                      // blocks of the cooperative kernel per multiprocessor
 constexpr int64_t kMostTogether = 16384;          // units that it takes

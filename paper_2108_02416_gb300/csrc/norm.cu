@@ -1,9 +1,9 @@
 // aspis_grad_norm: the global norm of many tensors, sqrt of the sum of all squares.
 //
 // One kernel reads every element once and is bound by HBM (1.1 billion bf16 values in 146 tensors, with each
-// one's own norm, 318 us: 7.2 TB/s) or, in small lists, by latency (six tensors 6.2 us, 62 of a
+// one's own norm, 314 us: 7.2 TB/s) or, in small lists, by latency (six tensors 6.2 us, 62 of a
 // ResNet-18 16.8).  Its last block to finish adds up the partial sums in their order: the result depends
-// on the lengths and the grid alone, not on which block finished first.  Units are dealt to warps in turn, and a
+// on the lengths, the addresses modulo 16 and the grid, not on which block finished first.  Units are dealt to warps in turn, and a
 // block leaves one partial sum.  Where the tensors' own norms are wanted, a block takes a
 // contiguous run of units and leaves one per tensor that it meets.  The (block, tensor) pairs that occur
 // then form a staircase (a later block starts no earlier than at the earlier one's last tensor), so
