@@ -316,6 +316,7 @@ few_kernel(const __grid_constant__ FewArgs a)
         }
         return;
     }
+    if constexpr (CLUSTER) cluster_begin();       // (the blocks above are whole clusters)
     const uint32_t rank = CLUSTER ? blockIdx.x : 0, mask = (1u << a.bits) - 1;
     const uint32_t begin = rank << a.tile_bits, size = begin < a.T ? min(1u << a.tile_bits, a.T - begin) : 0;
     // a warp has 32 * rounds neighbouring pairs
@@ -358,6 +359,7 @@ few_kernel(const __grid_constant__ FewArgs a)
         for (int w = 0; w < kSortWarps; ++w) count += n[w] = place[w][t];
         if constexpr (CLUSTER) {
             auto cluster = cg::this_cluster();
+            if (pass == 0) cluster_begun();
 #pragma unroll
             for (int b = 0; b < kRanks; ++b) cluster.map_shared_rank(digits[rank], b)[t] = (uint16_t)count;
             cluster.sync();                       // and all have their pairs in registers

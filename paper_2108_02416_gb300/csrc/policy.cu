@@ -260,8 +260,9 @@ hold_kernel(const __grid_constant__ Args a)
     const Row r = make_row<TYPE, MODE>(a, i);
     if (r.y < 0) {
         skip_row<TYPE, MODE>(a, r, rank * size + t, count * size);
-        return;
+        return;                                   // (in all blocks of a cluster)
     }
+    if constexpr (KIND == kCluster) cluster_begin();
     const float k = a.a * kLog2e;
     const Cut<int> cut(r.in, V, B);
     const int share = KIND == kCluster ? a.share : cut.groups, from = rank * share;
@@ -349,6 +350,7 @@ hold_kernel(const __grid_constant__ Args a)
     }
     if constexpr (KIND == kCluster) {
         auto cluster = cg::this_cluster();
+        cluster_begun();
         if (threadIdx.x < count) *cluster.map_shared_rank(&ranks[rank], threadIdx.x) = p;
         cluster.sync();
         if (warp == 0) p = join_lanes(lane < count ? ranks[lane] : nothing, 32, k);
