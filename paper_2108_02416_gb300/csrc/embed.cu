@@ -98,9 +98,9 @@ rows_kernel(const __grid_constant__ RowsArgs a)
         }
     } else {
         c0 -= behind<BO>(out);                    // a multiple of eight elements in memory
-        // columns counted from the share's first one, of which the row has lo .. hi - 1
-        const int64_t first = c0 - 8 * lane;
-        const int lo = first < 0 ? (int)-first : -8, hi = (int)min(a.cols - first, (int64_t)1 << 20);
+        const int64_t first = c0 - 8 * lane;      // the share's; columns are counted from it
+        const Columns columns = columns_from(first, a.cols, 1 << 20);
+        const int lo = columns.lo, hi = columns.hi;
         const uint64_t block = (number + c0) >> 3;
         const int pieces = min((int)a.pieces, (hi + kWidth - 1) / kWidth);
         const int sx = behind<BI>(x + c0 * BI), sr = KIND == kResidual ? behind<BO>(res + c0 * BO) : 0, off = (int)((number + c0) & 7);
@@ -115,8 +115,8 @@ rows_kernel(const __grid_constant__ RowsArgs a)
             if (i >= pieces) break;
             const int c = 8 * lane + i * kWidth;
             v[i] = {};
-            if (KIND != kEmbed || from >= 0) v[i] = load_around<IN, KIND == kEmbed>(x, c, sx, lo, hi, x_end);
-            if constexpr (KIND == kResidual) w[i] = load_around<OUT, false>(res, c, sr, lo, hi, res_end);
+            if (KIND != kEmbed || from >= 0) v[i] = load_around<IN, KIND == kEmbed>(x, c, sx, columns, x_end);
+            if constexpr (KIND == kResidual) w[i] = load_around<OUT, false>(res, c, sr, columns, res_end);
         }
 #pragma unroll
         for (int i = 0; i < P; ++i) {
@@ -158,6 +158,7 @@ cells_kernel(const __grid_constant__ RowsArgs a)
     const uint32_t all = (uint32_t)a.rows * a.chunks;             // (a.chunks: cells of a row)
     const uint64_t stream = mask_stream(a.mask);
     const int cols = (int)a.cols;
+    const Columns columns = {0, cols};
     uint32_t row[P];
     int64_t from[P];
     int c[P];
@@ -186,13 +187,13 @@ cells_kernel(const __grid_constant__ RowsArgs a)
             v[i][0] = v[i][1] = {};
             if (real) {
                 const bool x_end = a.ldx < 8 || (KIND == kEmbed ? from[i] <= 0 || from[i] + 1 >= a.V : end);
-                v[i][0] = load_around<IN, KIND == kEmbed>(x, c[i], sx, 0, cols, x_end);
-                if (sx) v[i][1] = load_around<IN, KIND == kEmbed>(x, c[i] + 8, sx, 0, cols, x_end);
+                v[i][0] = load_around<IN, KIND == kEmbed>(x, c[i], sx, columns, x_end);
+                if (sx) v[i][1] = load_around<IN, KIND == kEmbed>(x, c[i] + 8, sx, columns, x_end);
             }
             if constexpr (KIND == kResidual) {
                 const int sr = behind<BO>(res + c[i] * BO);
-                w[i][0] = load_around<OUT, false>(res, c[i], sr, 0, cols, end || a.ldr < 8);
-                if (sr) w[i][1] = load_around<OUT, false>(res, c[i] + 8, sr, 0, cols, end || a.ldr < 8);
+                w[i][0] = load_around<OUT, false>(res, c[i], sr, columns, end || a.ldr < 8);
+                if (sr) w[i][1] = load_around<OUT, false>(res, c[i] + 8, sr, columns, end || a.ldr < 8);
             }
         }
     }

@@ -432,8 +432,7 @@ struct Cells {
             if (8 * lane < n) r = load_group<TYPE, false>(p + 8 * lane * kBytes<TYPE>);
         } else {
             shift = behind<kBytes<TYPE>>(p);
-            const int right = (int)min(a.width - c0, (int64_t)512);
-            r = load_around<TYPE, false>(p, 8 * lane, shift, c0 ? -8 : 0, right, i == 0 || i + 1 == a.T || a.ld < 8);
+            r = load_around<TYPE, false>(p, 8 * lane, shift, columns_from(c0, a.width, 512), i == 0 || i + 1 == a.T || a.ld < 8);
         }
     }
     __device__ __forceinline__ void get(float (&f)[8]) const

@@ -3,6 +3,7 @@
 #pragma once
 
 #include "aspis_worker.h"
+#include "columns.h"
 #include "optim.cuh"
 
 namespace aspis {
@@ -145,18 +146,18 @@ __device__ __forceinline__ void store_edge(char *row, int c, int lo, int hi, con
         if (c + k >= lo && c + k < hi) store_elem<TYPE>(row, c + k, f[k]);
 }
 
-// The group of a row's elements lo .. hi - 1 that element c lies in, `shift` behind the group's begin; element by element
-// where the row is the matrix's first or last (`end`), as the group may reach out of that.
+// The group that element c of a row lies in, `shift` behind the group's begin, or what load_of leaves of it, with zeros.
 template <int TYPE, bool KEEP>
-__device__ __forceinline__ Raw<kBytes<TYPE>> load_around(const char *row, int c, int shift, int lo, int hi, bool end)
+__device__ __forceinline__ Raw<kBytes<TYPE>> load_around(const char *row, int c, int shift, Columns columns, bool end)
 {
     constexpr int B = kBytes<TYPE>;
     Raw<B> r = {};
     c -= shift;
-    if (c + 8 <= lo || c >= hi) return r;
-    if (!end || (c >= lo && c + 8 <= hi)) return load_group<TYPE, KEEP>(row + (int64_t)c * B);
+    const Load how = load_of(c, columns, end);
+    if (how == Load::none) return r;
+    if (how == Load::whole) return load_group<TYPE, KEEP>(row + (int64_t)c * B);
     float f[8];
-    load_edge<TYPE>(f, row, c, lo, hi);
+    load_edge<TYPE>(f, row, c, columns.lo, columns.hi);
 #pragma unroll
     for (int i = 0; i < 2 * B; ++i) {
         if constexpr (B == 4)
