@@ -157,7 +157,7 @@ __global__ void __launch_bounds__(kSortThreads)
 scatter_kernel(const __grid_constant__ SortArgs a)
 {
     __shared__ __align__(16) uint2 stage[kSubTile];
-    __shared__ uint16_t place[kSortWarps][kDigits];
+    __shared__ __align__(4) uint16_t place[kSortWarps][kDigits];   // (cleared by words)
     __shared__ uint32_t sums[kSortWarps], shift_of[kDigits];      // from the place in `stage` to that in `out`
     const int t = threadIdx.x, lane = t % 32, warp = t / 32;
     const uint32_t mask = (1u << a.bits) - 1;
@@ -292,7 +292,7 @@ few_kernel(const __grid_constant__ FewArgs a)
     namespace cg = cooperative_groups;
     constexpr int kRanks = CLUSTER ? 8 : 1;
     __shared__ uint2 tile[kSubTile];
-    __shared__ uint16_t place[kSortWarps][kDigits], digits[kRanks][kDigits];
+    __shared__ __align__(4) uint16_t place[kSortWarps][kDigits], digits[kRanks][kDigits];
     __shared__ uint32_t sums[kSortWarps];
     const int t = threadIdx.x, lane = t % 32, warp = t / 32;
     asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");

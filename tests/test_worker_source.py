@@ -39,3 +39,14 @@ def test_blocks_of_a_cluster_have_begun_before_their_memory_is_touched(file, nam
     before = text[: REMOTE.search(text).start()]
     arrived, waited = before.find("cluster_begin()"), before.find("cluster_begun()")
     assert 0 <= arrived < waited or "cluster_sync_all()" in before or "cluster.sync()" in before
+
+
+@pytest.mark.parametrize("file,name,text", KERNELS, ids=[f"{k[0]}-{k[1]}" for k in KERNELS])
+def test_shared_arrays_read_by_wider_words_are_aligned(file, name, text):
+    """An array of 16-bit or 8-bit elements in shared memory is aligned to its element alone unless it says more."""
+    for line in re.findall(r"__shared__[^;]*\buint(?:8|16)_t[^;]*;", text):
+        aligned = re.search(r"__align__\((\d+)\)", line)
+        for array in re.findall(r"(\w+)(?:\[[^\]]*\])+", line):
+            for wide in re.findall(r"reinterpret_cast<(?:const )?(\w+) \*>\(\s*&?" + array + r"\b", text):
+                need = {"uint32_t": 4, "uint2": 8, "uint4": 16, "float4": 16}[wide]
+                assert aligned and int(aligned.group(1)) >= need, (array, wide)
