@@ -122,15 +122,17 @@ rows_kernel(const __grid_constant__ RowsArgs a)
         for (int i = 0; i < P; ++i) {
             if (i >= pieces) break;
             const int c = 8 * lane + i * kWidth;
-            float f[8];
-            to_floats(with_next(v[i], sx), IN == ASPIS_BF16, f);
-            if (a.mask.threshold) {
-                Raw<2> words;
-                philox(words.w, a.mask, (block + (kWidth / 8) * i) & (~UINT64_C(0) >> 3), stream);
-                mask8(f, a.mask, with_next(words, off).w, a.factor);
-            } else
+            float f[8] = {};
+            if (KIND != kEmbed || from >= 0) {
+                to_floats(with_next(v[i], sx), IN == ASPIS_BF16, f);
+                if (a.mask.threshold) {
+                    Raw<2> words;
+                    philox(words.w, a.mask, (block + (kWidth / 8) * i) & (~UINT64_C(0) >> 3), stream);
+                    mask8(f, a.mask, with_next(words, off).w, a.factor);
+                } else
 #pragma unroll
-                for (int k = 0; k < 8; ++k) f[k] *= a.factor;
+                    for (int k = 0; k < 8; ++k) f[k] *= a.factor;
+            }
             if constexpr (KIND == kResidual) {
                 float g[8];
                 to_floats(with_next(w[i], sr), OUT == ASPIS_BF16, g);
