@@ -71,7 +71,8 @@ aspis_status aspis_dropout(const void *x, int x_type, int64_t ldx, const void *r
 /* out[i] = drop( scale * table[token_i] ) for i < T.
  *   table  [V][width], ld_table apart
  *   drop   or NULL; element (i, j) of out has number first + i * width + j
- *   scale  finite */
+ *   scale  finite; ASPIS_E_RANGE where drop leaves values and scale * 65536 / (65536 - t) is neither 0 nor a normal
+ *          number of fp32 */
 aspis_status aspis_embed(const void *table, int table_type, int64_t ld_table, int64_t V, const void *tokens,
                          int token_type, int64_t T, int64_t width, float scale, const aspis_drop *drop,
                          void *out, int out_type, int64_t ld_out, void *stream);
@@ -84,7 +85,7 @@ size_t aspis_embed_workspace_bytes(int64_t T, int64_t V, int64_t width);
  * and the tokens alone fix, rounded once.  Tokens are sorted (stably) and each run of equal ones is summed in pieces.
  *   accumulate  0: all V rows are written, zeros where no token is
  *               1: table_grad + the sum replaces it, in the rows that tokens name; no other is touched
- *   drop        as in aspis_embed, or NULL
+ *   scale, drop as in aspis_embed
  *   work        ASPIS_E_RANGE where work_bytes is too small
  * T, V < 2^31; T = 0 is allowed (grad, tokens and work may then be NULL). */
 aspis_status aspis_embed_grad(const void *grad, int grad_type, int64_t ld_grad, const void *tokens,

@@ -338,6 +338,7 @@ extern "C" aspis_status aspis_embed(const void *table, int table_type, int64_t l
     Rows in{table, V, width, ld_table, table_type}, to{out, T, width, ld_out, out_type}, none{};
     RowsArgs a{};
     aspis_status s = make_mask(drop, a.mask);
+    if (s == ASPIS_OK) s = make_factor(scale, a.mask, a.factor);
     if (s == ASPIS_OK) s = in.check();
     if (s == ASPIS_OK) s = to.check();
     if (s != ASPIS_OK) return s;
@@ -348,6 +349,5 @@ extern "C" aspis_status aspis_embed(const void *table, int table_type, int64_t l
     if (rows_meet(in, to) || ranges_meet(tokens, T * token_bytes, out, to.bytes())) return ASPIS_E_INVAL;
     a.tokens = tokens, a.V = V;
     a.wide_tokens = token_type == ASPIS_I64;
-    a.factor = scale * a.mask.up;
     return launch_rows(a, in, none, to, (cudaStream_t)stream);
 }

@@ -847,6 +847,7 @@ extern "C" aspis_status aspis_embed_grad(const void *grad, int grad_type, int64_
     SumArgs a{};
     Plan p;
     aspis_status s = make_mask(drop, a.mask);
+    if (s == ASPIS_OK) s = make_factor(scale, a.mask, a.factor);
     if (s == ASPIS_OK) s = in.check();
     if (s == ASPIS_OK) s = out.check();
     if (s != ASPIS_OK) return s;
@@ -934,7 +935,6 @@ extern "C" aspis_status aspis_embed_grad(const void *grad, int grad_type, int64_
     a.blocks = p.chunks * a.columns;
     a.fill_from = accumulate ? a.V : filled;
     a.fill_rows = group;
-    a.factor = scale * a.mask.up;
     cudaError_t e;
     switch (grad_type * 3 + table_type) {
         case 0: e = launch_types<0, 0>(a, eights, accumulate, st); break;

@@ -41,6 +41,14 @@ inline aspis_status make_mask(const aspis_drop *drop, Mask &m)
     return ASPIS_OK;
 }
 
+// scale times what stays is multiplied by: one fp32 number.  Where that product is infinite a value of 0 would become NaN, and where
+// it is below the normal numbers few of its bits are left: ASPIS_E_RANGE.
+inline aspis_status make_factor(float scale, const Mask &m, float &factor)
+{
+    factor = scale * m.up;
+    return m.threshold == 0 || factor == 0.0f || isnormal(factor) ? ASPIS_OK : ASPIS_E_RANGE;
+}
+
 // Philox 4x32 with ten rounds of (counter = block, stream; key): 128 bits, 16 for each of eight elements.  With 32
 // bits an element, two such calls, dropout is bound by its multiplications: 268 million bf16 values 228 us, with 16
 // bits 156, as long as a copy takes.

@@ -1,0 +1,24 @@
+"""Calls of include/aspis_worker.h that have no right answer, or none in fp32, are refused before anything is enqueued (CPU:
+addresses are fake and never read)."""
+import ctypes
+
+import pytest
+
+from test_worker_abi import AT, STEP, ap, embed, embed_grad
+
+
+def drop(p, step=None):
+    return ctypes.byref(ap._Drop(p, 1, 2, 0, step))
+
+
+@pytest.mark.parametrize("call", [embed, embed_grad])
+@pytest.mark.parametrize("scale,p,status", [
+    (2e38, 0.5, ap.E_RANGE), (-2e38, 0.5, ap.E_RANGE), (3.4028234e38, 2.0 ** -16, ap.E_RANGE), (6e33, 1 - 2.0 ** -16, ap.E_RANGE),
+    (1e-40, 0.5, ap.E_RANGE),                                    # a factor that few bits are left of
+    (2e38, 0.25, ap.OK), (5e33, 1 - 2.0 ** -16, ap.OK), (2e38, 0.0, ap.OK), (2e38, 1.0, ap.OK),
+    (1e-40, 0.0, ap.OK), (0.0, 0.5, ap.OK), (-1.5, 0.5, ap.OK)])
+def test_factors_beyond_the_range(call, scale, p, status):
+    """scale times what stays is multiplied by is one fp32 number; with no columns nothing is enqueued where it is allowed"""
+    assert call(scale=scale, drop=drop(p), width=0) == status
+    if status != ap.OK:
+        assert call(scale=scale, drop=drop(p)) == status
