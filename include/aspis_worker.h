@@ -121,7 +121,8 @@ typedef struct {
     float clip_low, clip_high;   /* rho is clipped to [1 - clip_low, 1 + clip_high]; in [0, 1] and >= 0, high may be infinite */
     float kl_coef;               /* beta, finite and >= 0; 0: k is summed, and has no other part */
     float scale;                 /* finite: 1 / the tokens of the whole batch, not of this file alone */
-    float grad_scale;            /* finite: a loss scale, which only dz is multiplied by */
+    float grad_scale;            /* finite: a loss scale, which only dz is multiplied by.  With grad, ASPIS_E_RANGE where
+                                    grad_scale * scale * logit_scale is neither 0 nor a normal number of fp32 */
 } aspis_policy_args;
 
 /* Device bytes that aspis_policy_loss needs for T tokens; 0 where T is out of range.  Host only. */

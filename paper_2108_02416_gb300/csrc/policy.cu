@@ -31,7 +31,7 @@ struct Args {
     float *logp;
     float4 *terms;                                // w (L + beta k), w L, w k, w [clipped] of a row
     int64_t T, V, ld, ld_grad;
-    float a, low, high, beta, scale, grad_scale;  // low, high: the bounds of the ratio
+    float a, low, high, beta, scale, factor;      // low, high: the bounds of the ratio; factor: grad_scale scale a
     int32_t wide_tokens;
     int32_t blocks, share;                        // that have a row: a cluster; groups of each (rows of any alignment)
     int32_t ahead;                                // rows whose blocks run at the same time
@@ -222,7 +222,7 @@ __device__ __forceinline__ float finish_row(const Args &a, const Row &r, const G
         a.terms[r.i] = make_float4(r.w * (a.beta > 0.0f && a.ref ? l.loss + a.beta * l.kl : l.loss), r.w * l.loss,
                                    r.w * l.kl, r.w * l.clipped);
     }
-    return a.grad_scale * a.scale * r.w * a.a * l.slope;
+    return a.factor * r.w * l.slope;
 }
 
 // The kernel that adds the rows' terms may be scheduled while this one runs; it waits for its end.
@@ -678,6 +678,9 @@ extern "C" aspis_status aspis_policy_loss(const aspis_policy_args *p, void *stre
     aspis_status s = check_rows(in, p->tokens, p->token_type, p->logit_scale);
     if (s == ASPIS_OK && p->grad) s = out.check();
     if (s != ASPIS_OK) return s;
+    // infinite, it would make NaN of a slope of 0; below the normal numbers it would have few bits
+    const float factor = (float)((double)p->grad_scale * p->scale * p->logit_scale);
+    if (p->grad && !isnormal(factor) && p->grad_scale != 0.0f && p->scale != 0.0f) return ASPIS_E_RANGE;
     const int64_t T = p->T, work = (int64_t)aspis_policy_workspace_bytes(T);
     if (!p->sums || (T > 0 && (!p->advantages || !p->work))) return ASPIS_E_INVAL;
     const float *const rows[] = {p->old_logp, p->ref_logp, p->advantages, p->weights, p->logp, p->sums};
@@ -706,7 +709,7 @@ extern "C" aspis_status aspis_policy_loss(const aspis_policy_args *p, void *stre
     a.terms = static_cast<float4 *>(p->work);
     a.T = T, a.V = p->V, a.ld = p->ld, a.ld_grad = p->ld_grad;
     a.a = p->logit_scale, a.low = 1.0f - p->clip_low, a.high = 1.0f + p->clip_high;
-    a.beta = p->kl_coef, a.scale = p->scale, a.grad_scale = p->grad_scale;
+    a.beta = p->kl_coef, a.scale = p->scale, a.factor = factor;
     a.wide_tokens = p->token_type == ASPIS_I64;
     const cudaStream_t st = (cudaStream_t)stream;
     if (T == 0) {

@@ -4,7 +4,7 @@ import ctypes
 
 import pytest
 
-from test_worker_abi import AT, STEP, ap, embed, embed_grad
+from test_worker_abi import AT, STEP, ap, embed, embed_grad, policy
 
 
 def drop(p, step=None):
@@ -22,3 +22,14 @@ def test_factors_beyond_the_range(call, scale, p, status):
     assert call(scale=scale, drop=drop(p), width=0) == status
     if status != ap.OK:
         assert call(scale=scale, drop=drop(p)) == status
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(scale=1e30, grad_scale=1e30), ap.E_RANGE), (dict(scale=-1e30, grad_scale=1e30), ap.E_RANGE),
+    (dict(scale=1e30, logit_scale=1e10), ap.E_RANGE), (dict(scale=1e-30, grad_scale=1e-12), ap.E_RANGE),
+    (dict(scale=1e30, grad_scale=1e30, grad=None), ap.E_ALIGN),  # nothing is multiplied by it
+    (dict(scale=1e30, grad_scale=0.0), ap.E_ALIGN), (dict(scale=1e-20, grad_scale=2.0 ** 60), ap.E_ALIGN),
+    (dict(scale=1e30, grad_scale=1e30, logit_scale=1e-25), ap.E_ALIGN)])
+def test_factors_of_the_loss(change, status):
+    """grad_scale * scale * logit_scale is one fp32 number; work's address stops the calls that are allowed"""
+    assert policy(work=AT + 9 * STEP + 8, **change) == status
