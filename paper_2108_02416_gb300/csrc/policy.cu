@@ -298,6 +298,7 @@ hold_kernel(const __grid_constant__ Args a)
         if (edge >= 0) ze = load_elem<TYPE>(r.in, edge);
         zy = load_elem<TYPE>(r.in, r.y);
     }
+    if constexpr (KIND == kCluster) cluster_begun();              // (while the loads are on their way)
 
     uint32_t top = kNothing<TYPE>;
 #pragma unroll
@@ -350,7 +351,6 @@ hold_kernel(const __grid_constant__ Args a)
     }
     if constexpr (KIND == kCluster) {
         auto cluster = cg::this_cluster();
-        cluster_begun();
         if (threadIdx.x < count) *cluster.map_shared_rank(&ranks[rank], threadIdx.x) = p;
         cluster.sync();
         if (warp == 0) p = join_lanes(lane < count ? ranks[lane] : nothing, 32, k);

@@ -197,7 +197,7 @@ __device__ __forceinline__ int64_t load_token(const void *tokens, int wide, int6
 // A block's shared memory is there for the others of its cluster only once it has begun, and being scheduled together does not
 // say that it has.  cluster_begin() tells the others; cluster_begun(), which comes before the first access, waits for them.  What
 // lies between them hides the barrier.  All threads of all blocks of the cluster call both, or neither.
-__device__ __forceinline__ void cluster_begin() { asm volatile("barrier.cluster.arrive.relaxed;\n" ::: "memory"); }
+__device__ __forceinline__ void cluster_begin() { asm volatile("barrier.cluster.arrive.relaxed;\n"); }
 __device__ __forceinline__ void cluster_begun() { asm volatile("barrier.cluster.wait;\n" ::: "memory"); }
 
 // ---- on the host
