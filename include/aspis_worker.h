@@ -96,7 +96,8 @@ aspis_status aspis_embed_grad(const void *grad, int grad_type, int64_t ld_grad, 
 /* logp[i] = a z_i[y_i] - log sum_j exp( a z_i[j] ), with the maximum taken out first; 0 for a
  * padding token.  logits [T][V], ld apart; a = logit_scale (1 / temperature), finite and > 0.
  * IEEE-754 through the formula: a logit of -infinity has probability 0, a row of nothing else, or with
- * a NaN or +infinity in it, gives NaN.  Never above 0.  T = 0 is allowed. */
+ * a NaN or +infinity in it, gives NaN.  Never above 0, and exactly 0 (with a gradient of 0 in aspis_policy_loss) where all but
+ * y_i have probability 0.  T = 0 is allowed. */
 aspis_status aspis_token_logp(const void *logits, int type, int64_t ld, const void *tokens, int token_type,
                               int64_t T, int64_t V, float logit_scale, float *logp, void *stream);
 

@@ -201,20 +201,31 @@ __device__ __forceinline__ void skip_row(const Args &a, const Row &r, int64_t t,
     }
 }
 
-// The row's log-probability and its terms; returns c, what the gradient is multiplied by.
+// What the row's elements become in the gradient: 2^(k z - c) * minus, and the token's own.
+struct Slope {
+    float minus, own;
+};
+
+// The row's log-probability and its terms, and its gradient's factors.
 template <int MODE>
-__device__ __forceinline__ float finish_row(const Args &a, const Row &r, const Given &given, const Part &p, float zy, bool first)
+__device__ __forceinline__ Slope finish_row(const Args &a, const Row &r, const Given &given, const Part &p, float zy, bool first)
 {
     const float k = a.a * kLog2e;
     const Base base(p.m, k);
     // from the difference to the maximum, which loses least (logits of 16 bits: nothing); the maximum's own exponent is what
-    // rounding left of k m - c
-    float lp = !base.far ? fmaf(a.a, zy - p.m, kLn2 * (fmaf(p.m, k, -base.c) - log2f(p.s)))
-                     : isinf(p.m) ? NAN : (zy == p.m ? 0.0f : a.a * (zy - p.m)) - logf(p.s);
+    // rounding left of k m - c.  Where it has more than half of the sum, the rest is taken by itself: nothing beside the
+    // maximum makes exactly 0, as 2^(k m - c) is the same number in the sum and here.
+    float lp;
+    if (!base.far) {
+        const float left = fmaf(p.m, k, -base.c), top = exp2_fast(left), rest = p.s - top;
+        lp = fmaf(a.a, zy - p.m, rest < top ? -log1pf(rest / top) : kLn2 * (left - log2f(p.s)));
+    } else {
+        lp = isinf(p.m) ? NAN : (zy == p.m ? 0.0f : a.a * (zy - p.m)) - logf(p.s);
+    }
     lp = lp > 0.0f ? 0.0f : lp;                   // (roundings; a NaN stays)
     if (MODE == kScore) {
         if (first) a.logp[r.i] = lp;
-        return 0.0f;
+        return {0.0f, 0.0f};
     }
     const Loss l = row_loss(a, given, lp);
     if (first) {
@@ -222,7 +233,9 @@ __device__ __forceinline__ float finish_row(const Args &a, const Row &r, const G
         a.terms[r.i] = make_float4(r.w * (a.beta > 0.0f && a.ref ? l.loss + a.beta * l.kl : l.loss), r.w * l.loss,
                                    r.w * l.kl, r.w * l.clipped);
     }
-    return a.factor * r.w * l.slope;
+    if (MODE != kGrad) return {0.0f, 0.0f};
+    const float c = a.factor * r.w * l.slope, part = 1.0f / p.s;
+    return {-c * part, c * ((p.s - weight(zy, p.m, base, k)) * part)};
 }
 
 // The kernel that adds the rows' terms may be scheduled while this one runs; it waits for its end.
@@ -243,7 +256,7 @@ hold_kernel(const __grid_constant__ Args a)
     namespace cg = cooperative_groups;
     constexpr int B = kBytes<TYPE>, size = KIND == kWarp ? 32 : THREADS;         // threads of a block that share a row
     __shared__ Part parts[THREADS / 32], ranks[8];
-    __shared__ float given[4];                    // m, c, -c / s, z_y
+    __shared__ float given[3];                    // m, and what finish_row gives
     const int t = threadIdx.x % size, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     next_may_start();
     int rank = 0, count = 1;
@@ -356,17 +369,15 @@ hold_kernel(const __grid_constant__ Args a)
         if (warp == 0) p = join_lanes(lane < count ? ranks[lane] : nothing, 32, k);
     }
     __syncwarp();                                 // the token's element is read everywhere before one is overwritten
-    float c = 0.0f, minus = 0.0f;
-    if (t < 32) {
-        c = finish_row<MODE>(a, r, known, p, zy, rank == 0 && t == 0);
-        minus = -c / p.s;
-    }
+    Slope slope = {};
+    if (t < 32) slope = finish_row<MODE>(a, r, known, p, zy, rank == 0 && t == 0);
     if constexpr (MODE == kGrad) {
         if constexpr (KIND != kWarp) {
-            if (t == 0) given[0] = p.m, given[1] = c, given[2] = minus, given[3] = zy;
+            if (t == 0) given[0] = p.m, given[1] = slope.minus, given[2] = slope.own;
             __syncthreads();
-            p.m = given[0], c = given[1], minus = given[2], zy = given[3];
+            p.m = given[0], slope.minus = given[1], slope.own = given[2];
         }
+        const float minus = slope.minus;
         const Base base(p.m, k);
         const float2 kk = {k, k}, cc = {-base.c, -base.c}, mm = {minus, minus};
         char *out = r.out + ((int64_t)cut.head + 8 * (from + t)) * B;
@@ -398,7 +409,7 @@ hold_kernel(const __grid_constant__ Args a)
         if (edge >= 0) store_elem<TYPE>(r.out, edge, weight(ze, p.m, base, k) * minus);
         // the token's own element, by the thread that has just written the others of its group
         const int y = (int)r.y, g = y < cut.head || y >= cut.tail ? -1 : (y - cut.head) / 8 - from;
-        if (edge == y || (g >= 0 && g < mine && g % size == t)) store_elem<TYPE>(r.out, y, fmaf(weight(zy, p.m, base, k), minus, c));
+        if (edge == y || (g >= 0 && g < mine && g % size == t)) store_elem<TYPE>(r.out, y, slope.own);
     }
 }
 
@@ -465,9 +476,9 @@ long_kernel(const __grid_constant__ Args a)
     if (t % 32 == 0) parts[t / 32] = p;
     __syncthreads();
     p = join_lanes(parts[t % 32], 32, k);
-    const float c = finish_row<MODE>(a, r, known, p, zy, t == 0);
+    const Slope slope = finish_row<MODE>(a, r, known, p, zy, t == 0);
     if constexpr (MODE == kGrad) {
-        const float minus = -c / p.s;
+        const float minus = slope.minus;
         const Base base(p.m, k);
         char *out = r.out + cut.head * B;
         const bool aligned = (uintptr_t)out % (8 * B) == 0;
@@ -485,7 +496,7 @@ long_kernel(const __grid_constant__ Args a)
         if (edge >= 0) store_elem<TYPE>(r.out, edge, weight(ze, p.m, base, k) * minus);
         const bool inside = r.y >= cut.head && r.y < cut.tail;
         if (edge == r.y || (inside && (r.y - cut.head) / 8 % kThreads == t))
-            store_elem<TYPE>(r.out, r.y, fmaf(weight(zy, p.m, base, k), minus, c));
+            store_elem<TYPE>(r.out, r.y, slope.own);
     }
 }
 

@@ -4,7 +4,8 @@ import math
 import pytest
 
 import _worker_reference as ref
-from test_gpu_worker import (BF16, DEV, F16, F32, I64, SEED, ap, gen, normal, place, same_bits, torch)
+from _worker_reference import U, close
+from test_gpu_worker import (BF16, DEV, F16, F32, I64, SEED, TYPES, ap, gen, normal, place, run_policy, same_bits, torch)
 
 pytestmark = pytest.mark.gpu
 
@@ -26,3 +27,37 @@ def test_padding_is_zero_bit_by_bit(kind, out_kind, scale):
                 out = place((T, D), out_kind, out_offset, pad)[1]
                 ap.aspis_embed(table, ids, out, scale=scale, drop=drop)
                 assert same_bits(out[dead], torch.zeros_like(out[dead]))
+
+
+@pytest.mark.parametrize("a", [1.0, 0.7])
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("V", [24, 3000, 20_001, 70_000, 300_000, 1_100_000])
+def test_the_only_token_that_is_left(V, kind, a):
+    """its log-probability and the row's gradient are exactly 0, whatever its logit"""
+    T = 4
+    logits = torch.full((T, V), -math.inf, dtype=kind, device=DEV)
+    tokens = torch.tensor([0, V - 1, V // 2, 13], device=DEV)
+    logits[torch.arange(T, device=DEV), tokens] = torch.tensor([-3.0, 7.125, 0.0, 1e4], device=DEV).to(kind)
+    got = run_policy(logits, tokens, None, normal((T,), F32, gen(V)), logit_scale=a, grad_scale=16.0)
+    out = torch.empty(T, device=DEV)
+    ap.aspis_token_logp(logits, tokens, out, logit_scale=a)
+    assert bool((out == 0).all()) and bool((got["logp"] == 0).all())
+    assert bool((got["grad"] == 0).all())
+
+
+@pytest.mark.parametrize("V", [24, 3000, 70_000])
+def test_probabilities_next_to_one(V):
+    """One other token is d below the maximum: lp = -log1p(e^-d), relative to itself within the exponent's roundings (d may be off
+    by 3 u d, its power by 2^-22), the quotient, the logarithm and the sum that the rest is taken out of (u of the whole, each)."""
+    d = torch.linspace(0.5, 14.0, 28, device=DEV)
+    T = len(d)
+    logits = torch.full((T, V), -math.inf, device=DEV)
+    tokens = torch.full((T,), V // 2, device=DEV)
+    logits[:, V // 2] = 3.0
+    logits[:, 1] = 3.0 - d
+    out = torch.empty(T, device=DEV)
+    ap.aspis_token_logp(logits, tokens, out)
+    gap = logits[:, V // 2].double() - logits[:, 1].double()
+    rest = torch.exp(-gap)
+    want = -torch.log1p(rest)
+    close(out, want, rest * (3 * U * gap + 2.0 ** -21 + 8 * U) + 4 * U)
