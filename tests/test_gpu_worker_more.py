@@ -1,11 +1,13 @@
 """More of dropout, the embedding with its gradient and the policy loss: what tests/test_gpu_worker.py does not reach."""
+import functools
 import math
 
 import pytest
 
 import _worker_reference as ref
-from _worker_reference import U, close
-from test_gpu_worker import (BF16, DEV, F16, F32, I64, SEED, TYPES, ap, gen, normal, place, run_policy, same_bits, torch)
+from _worker_reference import U, close, dropped
+from test_gpu_worker import (BF16, DEV, F16, F32, I32, I64, SEED, TYPES, ap, gen, normal, place, run_policy, same_bits, torch,
+                             untouched)
 
 pytestmark = pytest.mark.gpu
 
@@ -61,3 +63,147 @@ def test_probabilities_next_to_one(V):
     rest = torch.exp(-gap)
     want = -torch.log1p(rest)
     close(out, want, rest * (3 * U * gap + 2.0 ** -21 + 8 * U) + 4 * U)
+
+
+# ------------------------------------------------------------------ gradients of many tokens
+# Pieces of 32 positions a warp and the kernel that joins runs between blocks: from 304 blocks of 256 tokens and 248 columns on.
+
+
+@functools.lru_cache(maxsize=4)
+def mask(p, first, T, D):
+    return ref.factors(ap.Drop(p, SEED, 6, first), T, D).to(DEV) if p else None
+
+
+def long_sums(grad, ids, V, scale, f, old):
+    """The gradient in 64 bits, and a bound of its error that long runs do not widen: a summand goes through at most 32
+    additions in its piece, 8 in its block, n / 512 + 2 in its half of the run's n / 256 + 2 parts and one of the halves, of n summands
+    no more than n; then the factor, itself rounded, the product and the addition to what was there: four roundings."""
+    live = (ids >= 0) & (ids < V)
+    at, x = ids.long()[live], grad.double() if f is None else dropped(grad.double(), f)
+    zero = torch.zeros(V, x.shape[1], dtype=torch.float64, device=DEV)
+    total = zero.index_add(0, at, x[live]) * scale
+    size = zero.index_add(0, at, x[live].abs()) * abs(scale)
+    n = torch.bincount(at, minlength=V).double()[:, None]
+    tol = (torch.minimum(n, 43 + n / 512) + 4) * U * size + ref.TINY * (n > 0)
+    if old is not None:
+        total = total + old.double()
+        tol = torch.where(n > 0, tol + 2 * U * total.abs(), 0.0)
+    return total, tol
+
+
+def check_long(ids, grad, V, out_kind, p=0.0, first=16, accumulate=False, scale=1.0, offset=0, pad=0):
+    T, D = grad.shape
+    assert -(-T // 256) * -(-D // 248) >= 304
+    store, out = place((V, D), out_kind, offset, pad)
+    old = None
+    if accumulate:
+        out.copy_(normal((V, D), F32, gen(99)))
+        old = out.clone()
+    else:
+        out.fill_(math.nan)
+    buf = ap.EmbedBuffers(T, V, D, DEV)
+    buf.work.fill_(0xFF)
+    ap.aspis_embed_grad(grad, ids, out, buf.work, scale=scale, drop=ap.Drop(p, SEED, 6, first) if p else None, accumulate=accumulate)
+    close(out, *long_sums(grad, ids, V, float(torch.tensor(scale, dtype=F32)), mask(p, first, T, D), old))
+    untouched(store, out)
+    if accumulate:
+        named = torch.zeros(V, dtype=torch.bool, device=DEV)
+        named[ids.long()[(ids >= 0) & (ids < V)]] = True
+        assert same_bits(out[~named], old[~named])
+
+
+@pytest.mark.parametrize("T,V,D", [(78_001, 300, 24), (20_001, 997, 999), (40_000, 50_000, 264), (30_000, 60, 600), (77_900, 80_000, 33)])
+@pytest.mark.parametrize("p", [0.0, 0.2])
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("kind,out_kind", [(F32, F32), (BF16, F32), (F16, F32), (BF16, BF16), (F16, F16), (F32, BF16), (BF16, F16), (F16, BF16),
+                                           (F32, F16)])
+def test_long_batches(T, V, D, p, accumulate, kind, out_kind):
+    """types, masks, sums and additions; rows that begin anywhere and rows at multiples of 16 bytes"""
+    g = gen(T + V)
+    for ids_kind, offset, pad in ((I64, 0, 0), (I32, 1, 3), (I32, 0, 8)):
+        ids = ref.zipf_tokens(T, V, g, ids_kind, DEV)
+        grad = place((T, D), kind, offset, pad)[1]
+        grad.copy_(normal((T, D), F32, g))
+        check_long(ids, grad, V, out_kind, p, 16, accumulate, 1.3, offset, pad)
+
+
+@pytest.mark.parametrize("T,D", [(78_001, 24), (40_100, 264), (40_100, 261)])
+@pytest.mark.parametrize("p,accumulate", [(0.0, False), (0.3, True), (0.3, False)])
+@pytest.mark.parametrize("name", ["one", "two", "distinct", "padding", "mostly_padding", "last", "runs_96", "runs_256", "runs_700", "runs_10000", "one_after_many"])
+def test_long_batches_of_uneven_tokens(name, T, D, p, accumulate):
+    """runs inside a block, from block to block and over many blocks, from their first position on and within"""
+    V, at = 80_000, torch.arange(T, device=DEV)
+    if name.startswith("runs"):
+        ids = at // int(name[5:])
+    else:
+        ids = {"one": lambda: torch.full_like(at, 7), "two": lambda: at % 2 * 900, "padding": lambda: torch.full_like(at, -1),
+               "distinct": lambda: torch.randperm(V, device=DEV, generator=gen(1))[:T], "last": lambda: torch.full_like(at, V - 1),
+               "mostly_padding": lambda: torch.where(at % 50 == 49, 3, -1),
+               "one_after_many": lambda: torch.where(at < 1000, at, 1000)}[name]()
+    ids = ids[torch.randperm(T, device=DEV, generator=gen(2))]
+    check_long(ids, normal((T, D), BF16, gen(T)), V, F32, p, 16, accumulate)
+
+
+@pytest.mark.parametrize("first", [2 ** 64 - 16, 2 ** 64 - 5, 2 ** 35])
+@pytest.mark.parametrize("D", [24, 27])
+def test_long_masks_beyond_the_last_number(D, first):
+    T, V = 78_001, 3000
+    check_long(ref.zipf_tokens(T, V, gen(3), I64, DEV), normal((T, D), F32, gen(4)), V, F32, 0.4, first)
+
+
+@pytest.mark.parametrize("T,V,D", [(40_000, 3000, 264), (78_001, 100_000, 24)])
+def test_bits_of_long_batches_depend_on_tokens_alone(T, V, D):
+    g = gen(9)
+    ids, grad = ref.zipf_tokens(T, V, g, I32, DEV), normal((T, D), BF16, g)
+    drop, buf = ap.Drop(0.1, SEED, 6), ap.EmbedBuffers(T, V, D, DEV)
+    want = torch.empty(V, D, device=DEV)
+    ap.aspis_embed_grad(grad, ids, want, buf.work, drop=drop)
+    for offset, pad in ((0, 0), (1, 0), (5, 3), (0, 8)):
+        moved, out = place((T, D), BF16, offset, pad)[1], place((V, D), F32, offset, pad)[1]
+        moved.copy_(grad)
+        buf.work.fill_(offset)
+        ap.aspis_embed_grad(moved, ids.long(), out, buf.work, drop=drop)
+        assert same_bits(out, want)
+        out.zero_()
+        ap.aspis_embed_grad(moved, ids, out, buf.work, drop=drop, accumulate=True)
+        assert torch.equal(out, want)
+
+
+def test_long_batches_in_a_graph_and_on_two_streams():
+    """the bits of calls one after the other, with new tokens at each replay"""
+    T, V, D = 78_001, 5000, 40
+    jobs = []
+    for seed in (1, 2):
+        g = gen(seed)
+        jobs.append(dict(ids=ref.zipf_tokens(T, V, g, I32, DEV), dy=normal((T, D), BF16, g), dW=torch.zeros(V, D, device=DEV),
+                         work=ap.EmbedBuffers(T, V, D, DEV).work, s=torch.cuda.Stream()))
+    drop = ap.Drop(0.1, SEED)
+
+    def call(j, stream=None, accumulate=False):
+        ap.aspis_embed_grad(j["dy"], j["ids"], j["dW"], j["work"], drop=drop, accumulate=accumulate, stream=stream)
+
+    def twice(j, stream=None):
+        call(j, stream)
+        call(j, stream, True)
+    want = []
+    for j in jobs:
+        twice(j)
+        want.append(j["dW"].clone())
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for j in jobs:
+            twice(j, j["s"])
+    torch.cuda.synchronize()
+    assert all(same_bits(j["dW"], w) for j, w in zip(jobs, want))
+    j, graph = jobs[0], torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=j["s"]):
+        twice(j)
+    for ids in (j["ids"].flip(0).clone(), jobs[1]["ids"].clone()):
+        j["ids"].copy_(ids)
+        j["dW"].fill_(7.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed = j["dW"].clone()
+        twice(j)
+        assert same_bits(j["dW"], replayed)
