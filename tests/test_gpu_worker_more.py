@@ -6,7 +6,7 @@ import pytest
 
 import _worker_reference as ref
 from _worker_reference import U, close, dropped
-from test_gpu_worker import (BF16, DEV, F16, F32, I32, I64, SEED, TYPES, ap, gen, normal, place, run_policy, same_bits, torch,
+from test_gpu_worker import (BF16, DEV, F16, F32, I32, I64, SEED, TYPES, ap, gen, normal, place, policy_inputs, run_policy, same_bits, torch,
                              untouched)
 
 pytestmark = pytest.mark.gpu
@@ -207,3 +207,23 @@ def test_long_batches_in_a_graph_and_on_two_streams():
         replayed = j["dW"].clone()
         twice(j)
         assert same_bits(j["dW"], replayed)
+
+
+# ------------------------------------------------------------------ the loss
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("V", [1001, 2049, 4097, 8193, 10_241, 20_481, 32_769, 65_537, 100_003, 131_080, 262_153, 300_007, 530_000])
+def test_long_rows_in_place(V, kind):
+    """the gradient's bits where it takes the logits' place, at any alignment and distance; what lies around it stays"""
+    T = 5
+    for offset, pad in ((0, 0), (1, 6), (3, 0), (8, 8)):
+        logits, tokens, old, adv, prior, weights = policy_inputs(T, V, kind, gen(V), offset, pad, level=4.0)
+        tokens[0] = 0
+        k = dict(clip=(0.2, 0.3), grad_scale=256.0, ref_logp=prior, weights=weights, kl_coef=0.1)
+        want = run_policy(logits, tokens, old, adv, **k)
+        buffer, inside = place((T, V), kind, offset, pad)
+        inside.copy_(logits)
+        got = run_policy(inside, tokens, old, adv, grad=inside, **k)
+        assert all(same_bits(got[n], want[n]) for n in want)
+        untouched(buffer, inside)
