@@ -318,6 +318,7 @@ extern "C" aspis_status aspis_dropout(const void *x, int x_type, int64_t ldx, co
     if (s == ASPIS_OK && residual) s = res.check();
     if (s != ASPIS_OK) return s;
     if (rows == 0 || cols == 0) return ASPIS_OK;
+    if (step_in(a.mask, to)) return ASPIS_E_INVAL;
     if (rows_meet(in, to) && !same_rows(in, to)) return ASPIS_E_INVAL;
     if (residual && rows_meet(res, to) && !same_rows(res, to)) return ASPIS_E_INVAL;
     // rows without gaps are one row: their elements' numbers go on from row to row
@@ -343,6 +344,7 @@ extern "C" aspis_status aspis_embed(const void *table, int table_type, int64_t l
     if (s == ASPIS_OK) s = to.check();
     if (s != ASPIS_OK) return s;
     if (T == 0 || width == 0) return ASPIS_OK;
+    if (step_in(a.mask, to)) return ASPIS_E_INVAL;
     const int token_bytes = token_type == ASPIS_I64 ? 8 : 4;
     if (!tokens) return ASPIS_E_INVAL;
     if ((uintptr_t)tokens % token_bytes) return ASPIS_E_ALIGN;

@@ -855,12 +855,13 @@ extern "C" aspis_status aspis_embed_grad(const void *grad, int grad_type, int64_
     if (width == 0) return ASPIS_OK;
     const int token_bytes = token_type == ASPIS_I64 ? 8 : 4;
     if (T > 0) {
-        if (!tokens || !work) return ASPIS_E_INVAL;
+        if (!tokens || !work || step_in(a.mask, out)) return ASPIS_E_INVAL;
         if ((uintptr_t)tokens % token_bytes || (uintptr_t)work % 16) return ASPIS_E_ALIGN;
         if (work_bytes < p.bytes) return ASPIS_E_RANGE;
         if (rows_meet(in, out) || ranges_meet(tokens, T * token_bytes, table_grad, out.bytes()) ||
             ranges_meet(work, (int64_t)p.bytes, table_grad, out.bytes()) || ranges_meet(work, (int64_t)p.bytes, grad, in.bytes()) ||
-            ranges_meet(work, (int64_t)p.bytes, tokens, T * token_bytes))
+            ranges_meet(work, (int64_t)p.bytes, tokens, T * token_bytes) ||
+            (a.mask.threshold && ranges_meet(work, (int64_t)p.bytes, a.mask.step, 8)))
             return ASPIS_E_INVAL;
     } else if (accumulate) {
         return ASPIS_OK;

@@ -249,6 +249,16 @@ inline bool rows_meet(const Rows &a, const Rows &b)
     return off < a.cols * type_bytes(a.type) || ld - off < b.cols * type_bytes(b.type);
 }
 
+// true where the number that a mask's stream is counted up by lies in a row of what is written
+inline bool step_in(const Mask &m, const Rows &a)
+{
+    if (!m.threshold || !ranges_meet(m.step, 8, a.p, a.bytes())) return false;
+    const int64_t ld = a.ld * type_bytes(a.type);
+    int64_t off = (int64_t)((uintptr_t)m.step - (uintptr_t)a.p) % ld;
+    if (off < 0) off += ld;
+    return off < a.cols * type_bytes(a.type) || off + 8 > ld;
+}
+
 inline bool same_rows(const Rows &a, const Rows &b)
 {
     return a.p == b.p && a.type == b.type && (a.ld == b.ld || a.rows <= 1);

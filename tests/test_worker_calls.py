@@ -33,3 +33,21 @@ def test_factors_beyond_the_range(call, scale, p, status):
 def test_factors_of_the_loss(change, status):
     """grad_scale * scale * logit_scale is one fp32 number; work's address stops the calls that are allowed"""
     assert policy(work=AT + 9 * STEP + 8, **change) == status
+
+
+@pytest.mark.parametrize("step,p,status", [
+    (AT, 0.1, ap.E_INVAL), (AT + 64, 0.1, ap.E_INVAL), (AT + 3 * 320 + 248, 0.1, ap.E_INVAL),
+    (AT + 256, 0.1, ap.E_ALIGN), (AT + 312, 0.1, ap.E_ALIGN),   # between the rows
+    (AT + 4 * 320, 0.1, ap.E_ALIGN), (AT - 8, 0.1, ap.E_ALIGN), (AT, 0.0, ap.E_ALIGN)])   # (without a mask it is not read)
+def test_step_of_a_mask_that_is_written(step, p, status):
+    """What a call writes must not be what it reads; an address that comes after this check stops the calls that are allowed."""
+    from test_worker_abi import dropout
+    k = dict(drop=drop(p, step))
+    if status != ap.E_ALIGN:
+        assert dropout(x=AT + STEP, out=AT, ldo=80, **k) == status
+    assert embed(out=AT, out_type=0, T=4, ld_out=80, tokens=AT + STEP + (2 if status == ap.E_ALIGN else 0), table=AT + 2 * STEP, **k) == status
+    assert embed_grad(table_grad=AT, V=4, ld_table=80, grad=AT + 2 * STEP, work=AT + 3 * STEP + (8 if status == ap.E_ALIGN else 0), **k) == status
+
+
+def test_step_in_the_workspace():
+    assert embed_grad(drop=drop(0.1, AT + 3 * STEP + 64)) == ap.E_INVAL
