@@ -686,7 +686,8 @@ def aspis_adamw(params: ParamList, step: int, lr: float, betas=(0.9, 0.999), eps
 
 class Drop:
     """A dropout mask: which elements stay is a function of ``seed``, ``stream`` (+ ``step``, a CUDA int64 [1]
-    that is read when the kernel runs) and the element's number from ``first`` on, and of nothing else."""
+    that is read when the kernel runs) and the element's number from ``first`` on, and of nothing else.  A Drop does not
+    change: another mask is another Drop."""
 
     def __init__(self, p: float, seed: int, stream: int = 0, first: int = 0, step=None):
         for name, x in (("seed", seed), ("stream", stream), ("first", first)):
@@ -698,10 +699,12 @@ class Drop:
             import torch
             if not step.is_cuda or step.dtype not in (torch.int64, getattr(torch, "uint64", torch.int64)) or step.numel() != 1:
                 raise ValueError("step must be one CUDA int64")
-        self.p, self.seed, self.stream, self.first, self.step = p, seed, stream, first, step
-        self._index = None if step is None else step.get_device()
-        self._c = _Drop(p, seed, stream, first, None if step is None else step.data_ptr())
-        self._ref = ctypes.byref(self._c)
+        c = _Drop(p, seed, stream, first, None if step is None else step.data_ptr())
+        self.__dict__.update(p=p, seed=seed, stream=stream, first=first, step=step, _c=c, _ref=ctypes.byref(c),
+                             _index=None if step is None else step.get_device())
+
+    def __setattr__(self, name, value):
+        raise AttributeError(f"{name}: a Drop does not change, make another one")
 
 
 def _drop_on(drop, index):

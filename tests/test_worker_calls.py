@@ -51,3 +51,12 @@ def test_step_of_a_mask_that_is_written(step, p, status):
 
 def test_step_in_the_workspace():
     assert embed_grad(drop=drop(0.1, AT + 3 * STEP + 64)) == ap.E_INVAL
+
+
+@pytest.mark.parametrize("name,value", [("p", 0.5), ("seed", 2), ("stream", 3), ("first", 8), ("step", None)])
+def test_a_mask_does_not_change(name, value):
+    """its numbers are in the structure that the calls get: another value would not be seen there"""
+    d = ap.Drop(0.1, 1, 2, 0)
+    with pytest.raises(AttributeError):
+        setattr(d, name, value)
+    assert (d.p, d.seed, d.stream, d.first, d.step) == (0.1, 1, 2, 0, None)
