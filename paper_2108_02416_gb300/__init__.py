@@ -638,7 +638,7 @@ def _launch(name, x, index, stream, *args):
     else:
         own = getattr(getattr(stream, "device", None), "index", None)
         if index >= 0 and own is not None and own != index:
-            raise ValueError(f"stream must be on the list's device {index}, got {own}")
+            raise ValueError(f"stream must be on device {index}, got {own}")
         raw = _stream(stream)
     if index < 0 or index == x._current():
         status = getattr(lib, name)(*args, raw)

@@ -4,7 +4,7 @@ import ctypes
 
 import pytest
 
-from test_worker_abi import AT, STEP, ap, embed, embed_grad, policy
+from test_worker_abi import AT, STEP, Stream, ap, calls, calls_on, embed, embed_grad, policy  # noqa: F401
 
 
 def drop(p, step=None):
@@ -60,3 +60,11 @@ def test_a_mask_does_not_change(name, value):
     with pytest.raises(AttributeError):
         setattr(d, name, value)
     assert (d.p, d.seed, d.stream, d.first, d.step) == (0.1, 1, 2, 0, None)
+
+
+def test_a_stream_of_another_device_is_refused_by_what_it_is(calls):
+    """(these calls have no list)"""
+    for call in calls_on(0, Stream(1)):
+        with pytest.raises(ValueError, match="^stream must be on device 0, got 1$"):
+            call()
+    assert calls == []
