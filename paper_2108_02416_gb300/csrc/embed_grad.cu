@@ -31,7 +31,7 @@ template <bool EIGHTS>
 constexpr int kCols = EIGHTS ? 256 : 248;
 constexpr int kPiece = 32, kChunk = kPiece * kRowWarps;          // sorted positions of a warp, of a block
 constexpr int kJoinWarps = 2;
-constexpr int kFewPiece = 8, kFewBlocks = 304;    // where that makes few blocks
+constexpr int kFewPiece = 8, kFewBlocks = 2 * kSMs;    // where that makes few blocks
 constexpr int kFewTokens = 8 * kSubTile, kOneTokens = 1024;      // sorted by a cluster of eight blocks, by one block
 
 static_assert(kOneTokens <= kSubTile, "a block's pairs in shared memory");
@@ -281,7 +281,7 @@ __device__ __forceinline__ void zero_rows(char *first, int64_t ld_bytes, int64_t
     }
 }
 
-constexpr int kFillBlocks = 303, kFillRows = 32768;
+constexpr int kFillBlocks = 2 * kSMs - 1, kFillRows = 32768;
 static_assert(kFillRows <= 64 * kSubTile, "their bits where the pairs are");
 constexpr int64_t kFillBytes = 48 << 20;          // what is written while the cluster sorts
 
@@ -877,7 +877,7 @@ extern "C" aspis_status aspis_embed_grad(const void *grad, int grad_type, int64_
     a.arrived = (uint32_t *)(w + p.arrived);
     // rows that a warp writes zeros to at a time: some 12 KB of them, a power of two up to 32, and work for 16 warps a multiprocessor
     uint32_t group = 1;
-    while (group < 32 && 2 * group * width * type_bytes(table_type) <= 12288 && (int64_t)group * 2 * 16 * 152 <= V) group *= 2;
+    while (group < 32 && 2 * group * width * type_bytes(table_type) <= 12288 && (int64_t)group * 2 * 16 * kSMs <= V) group *= 2;
     if (T > 0 && p.few) {
         FewArgs o{};
         o.tokens = tokens;

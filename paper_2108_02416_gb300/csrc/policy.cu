@@ -21,7 +21,6 @@ using namespace aspis;
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr int kSMs = 152;
 constexpr int kScore = 0, kLoss = 1, kGrad = 2;   // what a kernel gives
 
 struct Args {

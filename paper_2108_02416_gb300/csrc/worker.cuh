@@ -9,6 +9,7 @@
 namespace aspis {
 
 constexpr int kRowThreads = 256, kRowWarps = kRowThreads / 32;
+constexpr int kSMs = 152;
 
 // ---- the dropout mask (aspis_drop)
 
