@@ -9,7 +9,8 @@ connection with dropout (aspis_dropout), logits, the clipped policy loss with a 
 gradient (aspis_policy_loss; log-probabilities before the step by aspis_token_logp), and the embedding's gradient
 (aspis_embed_grad), written straight into the row of copies that the server gets.  Masks are functions of the file and the
 step, and sums have a fixed order, so honest copies agree in every bit: aspis_round finds the adversaries, and AdamW
-steps on the aggregate."""
+steps on the aggregate.  (The order of a row's sum depends on the row's address modulo 32: logits are tensors of their own here, so every
+worker's begin at such a boundary.)"""
 from __future__ import annotations
 
 import os

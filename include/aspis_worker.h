@@ -11,9 +11,11 @@
  *
  * aspis_check compares the copies of a file's gradient bit by bit, so r workers that
  * compute the same file have to get the same bits.  All calls here give them: sums have
- * an order that the arguments fix (none depends on which block ends first; of the addresses, at most
- * their remainder modulo 32 matters, and that to the loss alone), and a dropout mask is a
+ * an order that the arguments fix (none depends on which block ends first), and a dropout mask is a
  * function of a seed, a stream and the element's number, of nothing that the device remembers.
+ * One thing is left to the caller: aspis_token_logp and aspis_policy_loss add a row's logits in an order that depends on its
+ * address modulo 32.  So a file's workers place its logits alike, each row at the same remainder (the same ld, and
+ * logits that begin at multiples of 32 bytes or equally far behind one); else honest copies may differ in last bits.
  *
  * Conventions, beside those of aspis.h:
  *   - Matrices are rows of `cols` elements of fp32, bf16 or fp16 (aspis_dtype), ld >= cols
@@ -29,6 +31,8 @@
  *   - work is device memory, 16-byte aligned, of at least the bytes that the call's
  *     ..._workspace_bytes gives.  Nothing in it has to be kept or cleared between calls; calls that may
  *     overlap on the GPU, and graphs that may replay at the same time, need one each.
+ *   - No call differentiates by itself: aspis_dropout on the gradient, aspis_embed_grad and aspis_policy_loss's grad are the backward
+ *     passes, which a program calls.
  *   - No call allocates, copies from the host or waits; all can be captured in a graph.
  */
 #ifndef ASPIS_WORKER_H

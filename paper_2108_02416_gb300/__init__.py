@@ -35,6 +35,9 @@ gradient a worker computes, with the same bits on every worker:
   aspis_embed_grad(grad, tokens, table_grad, work)   its gradient, by sorted tokens
   aspis_token_logp(logits, tokens, logp)         log-probabilities of tokens
   aspis_policy_loss(logits, tokens, ...)         clipped policy loss with KL, and d logits
+
+All calls take tensors as memory and record nothing for torch.autograd: outputs have no
+grad_fn, also where an input requires a gradient.  The backward passes are calls of their own.
 """
 from __future__ import annotations
 

@@ -6,8 +6,10 @@
 // Where the input's groups and the mask's blocks begin there too (EIGHTS), that is one load, one block of random bits and
 // one store.  Else it takes what its neighbour loaded and drew as well: groups and blocks overlap those of
 // the output by the same number of elements in the whole row.
-// 16,384 x 4096 bf16 with a residual 64.4 us (6.2 TB/s), 16,384 tokens x 2048 fp32 to bf16 with a mask 26.9 (4.6 TB/s of what it
-// cannot do without; its instructions), 20,001 unaligned rows of 1001 fp16 to fp32 28.7 (4.2 TB/s; its instructions).
+// 16,384 x 4096 bf16 with a residual 64.4 us (6.2 TB/s).  16,384 tokens x 2048 fp32 to bf16 take 26.9 with a mask and 24.5 without one
+// (4.6 and 5.0 TB/s of what they cannot do without), 20,001 unaligned rows of 1001 fp16 to fp32 29.1 (4.1 TB/s): neither HBM (35 and
+// 28 % of its time) nor the issue slots (64 %) are full there, as a warp loads first and computes then, and a multiprocessor's
+// warps overlap the two in part.
 #include <limits.h>
 
 #include "worker.cuh"
@@ -150,8 +152,8 @@ rows_kernel(const __grid_constant__ RowsArgs a)
 
 // Narrow rows: a thread has eight neighbouring elements of a row, of which `cells` are enough for one at any offset.  Where
 // groups or blocks overlap the output's it loads and draws both itself: with a warp for each row of 16 to 200 columns most lanes
-// had nothing to do.  Dropout of 40,000 bf16 rows, 16 columns 2.6 us (10.8 with a warp a row), 33: 4.9 (16.5), 255: 14.2 (24.8), 256:
-// 9.1 (11.4), 512: 15.5 (16.5), 1001: 47 (47.8); with the lookup 512: 18.2 (17.4).
+// had nothing to do.  Dropout of 40,000 bf16 rows in wider ones (inputs in turn), 16 columns 3.0 us (11.2 with a warp a row), 33: 4.8 (19.3),
+// 255: 17.3 (28.7), 256: 10.8 (13.2), 512: 17.7 (19.1), 1001: 51.2 (51.9); with the lookup 512: 19.1 either way.
 template <int IN, int OUT, int KIND, bool EIGHTS>
 __global__ void __launch_bounds__(kRowThreads)
 cells_kernel(const __grid_constant__ RowsArgs a)

@@ -7,8 +7,8 @@
 //
 // Bound by HBM: logits are read once and their gradient written once.  A row is held in registers by a warp, a block or a
 // cluster, from the one reading to the gradient; longer ones are read twice, the second time from L2.
-// 8192 x 131,072 bf16 with the gradient 648 us (6.3 TB/s), 2047 x 50,001 fp16 at odd addresses 77.5 (4.8 TB/s: 13 waves of
-// clusters, and what each waits for its sums), log-probabilities of 8192 x 32,000 bf16 82.5 (6.4 TB/s).
+// 8192 x 131,072 bf16 with the gradient 650 us (6.3 TB/s), 2047 x 50,001 fp16 at odd addresses 78.6 (4.7 TB/s: 13 waves of
+// clusters, and what each waits for its token and weight and for its sums), log-probabilities of 8192 x 32,000 bf16 83 (6.3 TB/s).
 // The terms of the sums go to the workspace row by row and are added by one more kernel in a fixed order.
 #include <cooperative_groups.h>
 #include <limits.h>
@@ -587,8 +587,8 @@ cudaError_t launch_hold(Args a, int blocks, cudaStream_t stream)
 }
 
 // Blocks of a row, of 16 or 10 warps, by what a multiprocessor's two or three blocks hold together (more blocks, which wait for
-// one another, have to hold a tenth more: 25,000 bf16 logits took 72 us in one block, 131 in seven of two warps); 0: eight
-// are too few.  4096 x 40,000 fp16 115.7 us in two of 10, 133 in two of 16; 2048 x 200,000 bf16 306 in seven, 320 in eight.
+// one another, have to hold a tenth more: 25,000 bf16 logits took 73 us in one block, 131 in seven of two warps); 0: eight
+// are too few.  4096 x 40,000 fp16 117 us in two of 10, 136 in two of 16; 2048 x 200,000 bf16 308 in seven, 322 in eight.
 struct Blocks {
     int blocks, warps;
 };
@@ -610,8 +610,8 @@ cudaError_t launch_rows(const Args &a, cudaStream_t stream)
 {
     constexpr int kHeld = 32 * 16 / kBytes<TYPE>;                                // a warp's groups
     const int64_t groups = a.V / 8, warps = (groups + kHeld - 1) / kHeld;        // at most; that hold a row
-    // as few warps as hold the row, for what they do not hold is not in flight: 9000 x 3000 bf16 25.2 us in two warps, 29.2 in
-    // four; x 10,000 61.8 in five, 67.7 in eight
+    // as few warps as hold the row, for what they do not hold is not in flight: 9000 x 3000 bf16 28.0 us in two warps, 32.7 in
+    // four; x 10,000 62.8 in five, 69.4 in eight (inputs in turn)
     if (warps <= 1) return launch_hold<TYPE, MODE, 128, kWarp>(a, 1, stream);
     if (warps <= 2) return launch_hold<TYPE, MODE, 64, kBlock>(a, 1, stream);
     if (warps <= 4) return launch_hold<TYPE, MODE, 128, kBlock>(a, 1, stream);
@@ -623,7 +623,7 @@ cudaError_t launch_rows(const Args &a, cudaStream_t stream)
         const Blocks c = cluster_of(groups, kHeld);
         if (c.warps == 16) return launch_hold<TYPE, MODE, 512, kCluster>(a, c.blocks, stream);
         if (c.warps == 10) return launch_hold<TYPE, MODE, 320, kCluster>(a, c.blocks, stream);
-        // a multiprocessor for each block: one row of 200,000 fp32 logits 31.5 us in long_kernel, 8.3 so
+        // a multiprocessor for each block: one row of 200,000 fp32 logits 31.5 us in long_kernel, 8.7 so
         if (warps <= 8 * 32) return launch_hold<TYPE, MODE, 1024, kCluster>(a, 8, stream);
     }
     long_kernel<TYPE, MODE><<<(unsigned)a.T, 1024, 0, stream>>>(a);
