@@ -227,3 +227,63 @@ def test_long_rows_in_place(V, kind):
         got = run_policy(inside, tokens, old, adv, grad=inside, **k)
         assert all(same_bits(got[n], want[n]) for n in want)
         untouched(buffer, inside)
+
+
+# ------------------------------------------------------------------ the largest sizes
+
+
+@pytest.mark.parametrize("V", [2 ** 27 + 5, 2 ** 31 - 1])
+@pytest.mark.parametrize("T", [500, 9000, 20_001])
+def test_rows_of_a_table_up_to_the_last_number(V, T):
+    """four passes of the sort; zeros to all rows but those that are named"""
+    ids = torch.randint(0, V, (T,), device=DEV, generator=gen(T))
+    ids[:6] = torch.tensor([0, V - 1, V, -1, 2 ** 31, 2 ** 32], device=DEV)
+    ids[T // 2:] = ids[: T - T // 2].clone()             # each twice
+    grad = normal((T, 1), F32, gen(1))
+    grad[grad == 0] = 1.0
+    real = (ids >= 0) & (ids < V)
+    rows, at = torch.unique(ids[real], return_inverse=True)
+    x = grad[:, 0].double()[real]
+    want = torch.zeros(len(rows), dtype=torch.float64, device=DEV).index_add(0, at, x)
+    size = torch.zeros(len(rows), dtype=torch.float64, device=DEV).index_add(0, at, x.abs())
+    n = torch.bincount(at).double()
+    out = torch.full((V, 1), 7.0, dtype=BF16, device=DEV)
+    buf = ap.EmbedBuffers(T, V, 1, DEV)
+    ap.aspis_embed_grad(grad, ids, out, buf.work)
+    close(out[rows, 0], want, (n + 4) * U * size + ref.TINY)
+    assert sum(int(torch.count_nonzero(p)) for p in out.view(-1).split(2 ** 28)) == int(torch.count_nonzero(out[rows]))
+    out.fill_(0.5)
+    ap.aspis_embed_grad(grad, ids, out, buf.work, accumulate=True)
+    close(out[rows, 0], 0.5 + want, (n + 6) * U * (size + 0.5))
+    out[rows] = 0.5
+    assert all(bool((p == 0.5).all()) for p in out.view(-1).split(2 ** 28))
+
+
+@pytest.mark.parametrize("T,V,D", [(3_000_001, 1000, 1), (1_000_000, 1, 7)])
+def test_millions_of_tokens(T, V, D):
+    check_long(ref.zipf_tokens(T, V, gen(T), I32, DEV), normal((T, D), BF16, gen(1)), V, F32)
+
+
+@pytest.mark.parametrize("D,offset", [(3_000_008, 0), (3_000_001, 1)])
+def test_rows_of_millions_of_columns(D, offset):
+    T, V = 5, 3
+    ids = torch.tensor([1, -1, 0, 1, 3], device=DEV)
+    table = place((V, D), BF16, offset)[1]
+    table.copy_(normal((V, D), F32, gen(1)))
+    drop = ap.Drop(0.2, SEED, 6, 8)
+    f = ref.factors(drop, T, D).to(DEV)
+    buffer, out = place((T, D), F32, offset)
+    ap.aspis_embed(table, ids, out, drop=drop)
+    real = ((ids >= 0) & (ids < V))[:, None]
+    want = dropped(torch.where(real, table[ids.clamp(0, V - 1)].double(), 0.0), f)
+    close(out, want, 3 * U * want.abs() + ref.TINY)
+    untouched(buffer, out)
+    grad = torch.empty(V, D, device=DEV)
+    ap.aspis_embed_grad(out, ids, grad, ap.EmbedBuffers(T, V, D, DEV).work, drop=drop)
+    close(grad, *ref.embed_grad(out, ids, V, 1.0, f))
+    logits, tokens = table[:2].clone(), torch.tensor([D - 1, 0], device=DEV)
+    adv = normal((2,), F32, gen(2))
+    want, tol = ref.policy(logits, tokens, None, adv, grad_scale=1024.0)
+    got = run_policy(logits, tokens, None, adv, grad_scale=1024.0)
+    for name in ("sums", "logp", "grad"):
+        close(got[name], want[name], tol[name])
