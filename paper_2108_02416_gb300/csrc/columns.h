@@ -22,14 +22,10 @@ ASPIS_BOTH Columns columns_from(int64_t first, int64_t cols, int most)
     return {first > 0 ? -8 : (int)-first, (int)(cols - first < most ? cols - first : most)};
 }
 
-// How columns c .. c + 7 are loaded: not at all where the row has none of them; element by element where the row is the
-// matrix's first or last (`end`) and the group reaches out of it; else whole, neighbouring rows' elements with them.
-enum class Load { none, elements, whole };
-
-ASPIS_BOTH Load load_of(int c, Columns row, bool end)
-{
-    if (c + 8 <= row.lo || c >= row.hi) return Load::none;
-    return !end || (c >= row.lo && c + 8 <= row.hi) ? Load::whole : Load::elements;
-}
+// How columns c .. c + 7 are loaded: not at all where the row has none of them; whole, neighbouring rows' elements with them, where
+// no element of the group lies outside the matrix, as it may where the row is the first or last (`end`); else element by
+// element.  (Two conditions: as an enumeration of three the unaligned dropout of 20,001 x 1001 took 30.0 us, 28.8 so.)
+ASPIS_BOTH bool load_nothing(int c, Columns row) { return c + 8 <= row.lo || c >= row.hi; }
+ASPIS_BOTH bool load_whole(int c, Columns row, bool end) { return !end || (c >= row.lo && c + 8 <= row.hi); }
 
 }  // namespace aspis

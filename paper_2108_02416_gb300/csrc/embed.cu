@@ -7,7 +7,7 @@
 // one store.  Else it takes what its neighbour loaded and drew as well: groups and blocks overlap those of
 // the output by the same number of elements in the whole row.
 // 16,384 x 4096 bf16 with a residual 64.4 us (6.2 TB/s).  16,384 tokens x 2048 fp32 to bf16 take 26.9 with a mask and 24.5 without one
-// (4.6 and 5.0 TB/s of what they cannot do without), 20,001 unaligned rows of 1001 fp16 to fp32 29.1 (4.1 TB/s): neither HBM (35 and
+// (4.6 and 5.0 TB/s of what they cannot do without), 20,001 unaligned rows of 1001 fp16 to fp32 28.7 (4.2 TB/s): neither HBM (35 and
 // 28 % of its time) nor the issue slots (64 %) are full there, as a warp loads first and computes then, and a multiprocessor's
 // warps overlap the two in part.
 #include <limits.h>

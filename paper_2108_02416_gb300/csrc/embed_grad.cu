@@ -9,7 +9,7 @@
 // the workspace.  So long runs (a text's commonest token is a tenth of it) and tokens that occur once cost
 // the same, and the order of a sum depends on the tokens and the sizes alone.
 // Bound by HBM where T is large: 131,072 tokens x 2048 bf16 added to fp32 201 us, 172 of it the sums (6.2 TB/s), the
-// rest the sort in three launches and the joins.  Not where they go through a mask (x 1024 133 us, 90 without; x 1001 230 and 137): a
+// rest the sort in three launches and the joins.  Not where they go through a mask (x 1024 133 us, 90 without; x 1001 223 and 130): a
 // row's words are drawn after the row has arrived, so that both times add up; nor where rows are narrow (x 16 39 us: the sort).  8192 x 1024 with a mask into 32,000 rows 33 us (131 MB of it zeros and sums
 // written: 19), half of which is the latency of two launches and of the sums' last joins.
 #include <cooperative_groups.h>

@@ -155,16 +155,15 @@ __device__ __forceinline__ void store_edge(char *row, int c, int lo, int hi, con
         if (c + k >= lo && c + k < hi) store_elem<TYPE>(row, c + k, f[k]);
 }
 
-// The group that element c of a row lies in, `shift` behind the group's begin, or what load_of leaves of it, with zeros.
+// The group that element c of a row lies in, `shift` behind the group's begin, or the columns of it that the row has, and zeros.
 template <int TYPE, bool KEEP>
 __device__ __forceinline__ Raw<kBytes<TYPE>> load_around(const char *row, int c, int shift, Columns columns, bool end)
 {
     constexpr int B = kBytes<TYPE>;
     Raw<B> r = {};
     c -= shift;
-    const Load how = load_of(c, columns, end);
-    if (how == Load::none) return r;
-    if (how == Load::whole) return load_group<TYPE, KEEP>(row + (int64_t)c * B);
+    if (load_nothing(c, columns)) return r;
+    if (load_whole(c, columns, end)) return load_group<TYPE, KEEP>(row + (int64_t)c * B);
     float f[8];
     load_edge<TYPE>(f, row, c, columns.lo, columns.hi);
 #pragma unroll

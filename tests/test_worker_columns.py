@@ -22,9 +22,10 @@ using std::min;
 // `ld` apart; the matrix has elements 0 .. size - 1.
 static bool touch(std::vector<char> &seen, int64_t row_at, int64_t first, int c, Columns columns, bool end, int64_t size)
 {
-    const Load how = load_of(c, columns, end);
+    if (load_nothing(c, columns)) return true;
+    const bool whole = load_whole(c, columns, end);
     for (int k = 0; k < 8; ++k) {
-        if (how == Load::none || (how == Load::elements && (c + k < columns.lo || c + k >= columns.hi))) continue;
+        if (!whole && (c + k < columns.lo || c + k >= columns.hi)) continue;
         const int64_t at = row_at + first + c + k;
         if (at < 0 || at >= size) return false;
         seen[at] = 1;
