@@ -217,7 +217,9 @@ __device__ __forceinline__ Slope finish_row(const Args &a, const Row &r, const G
     float lp;
     if (!base.far) {
         const float left = fmaf(p.m, k, -base.c), top = exp2_fast(left), rest = p.s - top;
-        lp = fmaf(a.a, zy - p.m, rest < top ? -log1pf(rest / top) : kLn2 * (left - log2f(p.s)));
+        float share = kLn2 * (left - log2f(p.s)); // the maximum's log-probability
+        if (rest < top) share = -log1pf(rest / top);
+        lp = fmaf(a.a, zy - p.m, share);
     } else {
         lp = isinf(p.m) ? NAN : (zy == p.m ? 0.0f : a.a * (zy - p.m)) - logf(p.s);
     }
